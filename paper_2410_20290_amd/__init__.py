@@ -2,7 +2,7 @@
 
 Argument marshalling only: every step of the hot path runs in the library's
 HIP kernels.  torch provides device memory and streams.  The names follow the
-C interface in include/specrej.h.  Importing this module does not need a GPU;
+C interface in include/specrej.h and include/specrej_ops.h.  Importing this module does not need a GPU;
 calling anything that launches work does, and fails loudly if the library is
 not built.
 """
@@ -115,6 +115,28 @@ def lib():
                                            _i32, _vp, _vp]
         L.sr_correlation.argtypes = [_vp, _vp, _i32, P(ctypes.c_double), P(ctypes.c_double)]
         L.sr_improvement_score.argtypes = [_vp, _i32, _f32, P(ctypes.c_double)]
+        sz = ctypes.c_size_t
+        L.sr_page_fork.argtypes = [_vp, _vp, _i32, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
+        L.sr_page_reserve.argtypes = [_vp, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp,
+                                      _i32, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]
+        L.sr_page_reserve_scratch.argtypes = [_i32, _i32, _i32]
+        L.sr_page_compact.argtypes = [_vp, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp,
+                                      _vp, _vp, _vp, sz, _vp]
+        L.sr_page_compact_scratch.argtypes = [_i32]
+        L.sr_rope_frequencies.argtypes = [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp]
+        L.sr_page_append.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32,
+                                     _vp, _i32, _vp, _vp, _vp, _vp]
+        L.sr_paged_attention.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp,
+                                         _vp, _i32, _i32, _i32, _i32, _vp, _vp, sz, _vp]
+        L.sr_paged_attention_scratch.argtypes = [_i32] * 12
+        L.sr_token_logprobs.argtypes = [_i32, _vp, _i64, _i32, _i32, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, sz, _vp]
+        L.sr_token_logprobs_scratch.argtypes = [_i32, _i32, _i32]
+        for f in ("sr_page_reserve_scratch", "sr_page_compact_scratch", "sr_paged_attention_scratch",
+                  "sr_token_logprobs_scratch"):
+            getattr(L, f).restype = sz
+        for f in ("sr_page_fork", "sr_page_reserve", "sr_page_compact", "sr_rope_frequencies", "sr_page_append",
+                  "sr_paged_attention", "sr_token_logprobs"):
+            getattr(L, f).restype = _i32
         for f in ("sr_projection", "sr_decode_attention", "sr_decode_attention_noalloc", "sr_prefill_attention", "sr_plan_for_memory",
                   "sr_correlation", "sr_improvement_score", "sr_workspace_size", "sr_generate", "sr_philox_fill", "sr_sample", "sr_select", "sr_compact",
                   "sr_logits_teacher_forced", "sr_reward_scores"):
@@ -388,3 +410,202 @@ def reward_scores(gen: DeviceModel, rm: DeviceModel, prompt, p: sr_params, token
                                   len(prompt), ctypes.byref(p), _ptr(tokens), _ptr(lens), rows, max_len, _ptr(out),
                                   ws.ptr, ws.nbytes, _stream(stream)))
     return out
+
+
+# ------------------------------------- operators over a paged candidate cache
+# (include/specrej_ops.h).  Tensors are contiguous and on one GPU, which need
+# not be the current one; scratch belongs to the stream of the call.
+SR_ROPE_PLAIN, SR_ROPE_LINEAR, SR_ROPE_BANDS = 0, 1, 2
+
+
+def _expect(t, name: str, dtypes, shape=None):
+    """t's checks: type, layout and (None: any size) shape."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has type {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+
+
+def _call(tensors, stream, call, need=0, scratch_type=None):
+    """call(stream, scratch) on the tensors' device; scratch: `need` elements
+    of scratch_type, allocated on that stream (None when need is 0)."""
+    import torch
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors are on different devices")
+    if stream is not None and stream.device != dev:
+        raise ValueError("the stream is another device's")
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call(tensors, stream, call, need, scratch_type)
+    scratch = None
+    if need:
+        if stream is None:
+            scratch = torch.empty(need, dtype=scratch_type, device=dev)
+        else:
+            with torch.cuda.stream(stream):
+                scratch = torch.empty(need, dtype=scratch_type, device=dev)
+    _check(call(_stream(stream), _ptr(scratch)))
+
+
+def _cache_types():
+    import torch
+    return (torch.float32, torch.bfloat16, torch.int16)
+
+
+def _pool_args(pool):
+    """(ctypes arguments, n_pages) of a pool [layers][2][n_pages][hkv][page_tokens][hd]."""
+    _expect(pool, "pool", _cache_types(), (None, 2, None, None, None, None))
+    nl, _, n_pages, hkv, pt, hd = pool.shape
+    return (_ptr(pool), n_pages * hkv * pt * hd, nl, hkv, hd, pool.element_size(), pt, n_pages), n_pages
+
+
+def page_fork(table, lens, parent, page_tokens: int, table_out, lens_out, refs_out, window: int = 0, sinks: int = 0,
+              stream=None):
+    """sr_page_fork: table int32 [rows][max_pages], lens [rows], parent [new
+    rows] -> table_out [new rows][max_pages], lens_out, refs_out [n_pages]."""
+    import torch
+    i32 = (torch.int32,)
+    _expect(table, "table", i32, (None, None))
+    rows, mp = table.shape
+    _expect(lens, "lens", i32, (rows,))
+    _expect(parent, "parent", i32, (None,))
+    n = parent.shape[0]
+    _expect(table_out, "table_out", i32, (n, mp))
+    _expect(lens_out, "lens_out", i32, (n,))
+    _expect(refs_out, "refs_out", i32, (None,))
+    _call((refs_out, table, lens, parent, table_out, lens_out), stream, lambda s, _: lib().sr_page_fork(
+        _ptr(table), _ptr(lens), rows, mp, _ptr(parent), n, page_tokens, refs_out.shape[0], window, sinks,
+        _ptr(table_out), _ptr(lens_out), _ptr(refs_out), s))
+
+
+def page_reserve(pool, table, lens, refs, n_add, table_out, lens_out, refs_out, granted, info, stream=None):
+    """sr_page_reserve: room for n_add tokens (int32 [rows], or one number for
+    every row).  table_out, lens_out and refs_out may be the inputs."""
+    import torch
+    i32 = (torch.int32,)
+    pa, n_pages = _pool_args(pool)
+    _expect(table, "table", i32, (None, None))
+    rows, mp = table.shape
+    for t, name, shape in ((lens, "lens", (rows,)), (refs, "refs", (n_pages,)), (table_out, "table_out", (rows, mp)),
+                           (lens_out, "lens_out", (rows,)), (refs_out, "refs_out", (n_pages,)),
+                           (granted, "granted", (rows,)), (info, "info", (4,))):
+        _expect(t, name, i32, shape)
+    each = n_add if torch.is_tensor(n_add) else None
+    if each is not None:
+        _expect(each, "n_add", i32, (rows,))
+    need = int(lib().sr_page_reserve_scratch(rows, mp, n_pages))
+    _call((pool, table, lens, refs, each, table_out, lens_out, refs_out, granted, info), stream,
+          lambda s, w: lib().sr_page_reserve(*pa, _ptr(table), _ptr(lens), _ptr(refs), rows, mp, _ptr(each),
+                                             0 if each is not None else int(n_add), _ptr(table_out), _ptr(lens_out),
+                                             _ptr(refs_out), _ptr(granted), _ptr(info), w, need, s), need, torch.int32)
+
+
+def page_compact(pool, table, lens, refs, table_out, refs_out, info, stream=None):
+    """sr_page_compact: live pages to the front of the pool, in place.
+    table_out and refs_out may be the inputs."""
+    import torch
+    i32 = (torch.int32,)
+    pa, n_pages = _pool_args(pool)
+    _expect(table, "table", i32, (None, None))
+    rows, mp = table.shape
+    for t, name, shape in ((lens, "lens", (rows,)), (refs, "refs", (n_pages,)), (table_out, "table_out", (rows, mp)),
+                           (refs_out, "refs_out", (n_pages,)), (info, "info", (4,))):
+        _expect(t, name, i32, shape)
+    need = int(lib().sr_page_compact_scratch(n_pages))
+    _call((pool, table, lens, refs, table_out, refs_out, info), stream,
+          lambda s, w: lib().sr_page_compact(*pa, _ptr(table), _ptr(lens), _ptr(refs), rows, mp, _ptr(table_out),
+                                             _ptr(refs_out), _ptr(info), w, need, s), need, torch.int32)
+
+
+def rope_frequencies(rot_dim: int, theta: float, scaling: int = SR_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                     high: float = 4.0, n: float = 8192.0) -> np.ndarray:
+    """sr_rope_frequencies: float64 [rot_dim / 2], radians a position."""
+    out = np.zeros(max(1, rot_dim // 2))
+    _check(lib().sr_rope_frequencies(rot_dim, theta, scaling, factor, low, high, n, out.ctypes.data))
+    return out
+
+
+def _layer_args(kpool, vpool, table, lens, n_new):
+    """(dtype, rows, max_pages, hkv, page_tokens, hd, n_pages) of one layer's
+    blocks [n_pages][hkv][page_tokens][hd] and the rows' table."""
+    import torch
+    i32 = (torch.int32,)
+    _expect(kpool, "kpool", _cache_types(), (None, None, None, None))
+    _expect(vpool, "vpool", (kpool.dtype,), tuple(kpool.shape))
+    _expect(table, "table", i32, (None, None))
+    rows, mp = table.shape
+    _expect(lens, "lens", i32, (rows,))
+    if n_new is not None:
+        _expect(n_new, "n_new", i32, (rows,))
+    n_pages, hkv, pt, hd = kpool.shape
+    return SR_F32 if kpool.dtype == torch.float32 else SR_BF16, rows, mp, hkv, pt, hd, n_pages
+
+
+def page_append(qkv, freqs, table, lens, kpool, vpool, q, n_new=None, interleaved: bool = False, stream=None):
+    """sr_page_append: qkv float [rows][lr][(hq + 2 hkv) hd], freqs float64
+    [rot_dim / 2] (None: no rotation) -> q float [rows][lr][hq][hd] and the
+    rows' pages of one layer's kpool, vpool [n_pages][hkv][page_tokens][hd]."""
+    import torch
+    dtype, rows, mp, hkv, pt, hd, n_pages = _layer_args(kpool, vpool, table, lens, n_new)
+    _expect(q, "q", (torch.float32,), (rows, None, None, hd))
+    lr, hq = q.shape[1:3]
+    _expect(qkv, "qkv", (torch.float32,), (rows, lr, (hq + 2 * hkv) * hd))
+    rot = 0
+    if freqs is not None:
+        _expect(freqs, "freqs", (torch.float64,), (None,))
+        rot = 2 * freqs.shape[0]
+    _call((qkv, freqs, table, lens, kpool, vpool, q, n_new), stream,
+          lambda s, _: lib().sr_page_append(dtype, hd, hq, hkv, rows, lr, _ptr(qkv), _ptr(freqs), rot, int(interleaved),
+                                            _ptr(kpool), _ptr(vpool), pt, n_pages, _ptr(table), mp, _ptr(lens),
+                                            _ptr(n_new), _ptr(q), s))
+
+
+def paged_attention(q, kpool, vpool, table, lens, out, n_new=None, window: int = 0, sinks: int = 0, shared: int = 0,
+                    max_len: int = None, stream=None):
+    """sr_paged_attention: q float [rows][lr][hq][hd], one layer's kpool, vpool
+    [n_pages][hkv][page_tokens][hd] -> out [rows][lr][hq*hd] in the cache's
+    type (bf16 may travel as int16).  max_len None: the table's capacity."""
+    import torch
+    dtype, rows, mp, hkv, pt, hd, n_pages = _layer_args(kpool, vpool, table, lens, n_new)
+    _expect(q, "q", (torch.float32,), (rows, None, None, hd))
+    lr, hq = q.shape[1:3]
+    _expect(out, "out", (torch.float32,) if dtype == SR_F32 else (torch.bfloat16, torch.int16), (rows, lr, hq * hd))
+    if max_len is None:
+        max_len = mp * pt
+    need = int(lib().sr_paged_attention_scratch(dtype, hd, hq, hkv, rows, lr, pt, mp, window, sinks, shared, max_len))
+    _call((q, kpool, vpool, table, lens, out, n_new), stream,
+          lambda s, w: lib().sr_paged_attention(dtype, hd, hq, hkv, rows, lr, _ptr(q), _ptr(kpool), _ptr(vpool), pt,
+                                                n_pages, _ptr(table), mp, _ptr(lens), _ptr(n_new), window, sinks,
+                                                shared, max_len, _ptr(out), w, need, s), need, torch.float32)
+
+
+def token_logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=None, temperature: float = 1.0,
+                   stream=None):
+    """sr_token_logprobs: logits [rows][vocab] (rows may be strided; float or
+    bf16, which may travel as int16), tokens int32 [rows] -> logprob, entropy
+    float [rows], top_ids int32 and top_logprobs float [rows][top]; any output
+    may be None."""
+    import torch
+    if logits.dtype not in _cache_types() or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: type {logits.dtype}, shape {tuple(logits.shape)}, strides {logits.stride()}")
+    rows, vocab = logits.shape
+    stride = logits.stride(0) if rows > 1 else vocab
+    top = top_ids.shape[-1] if top_ids is not None else top_logprobs.shape[-1] if top_logprobs is not None else 0
+    for t, name, typ, shape in ((tokens, "tokens", torch.int32, (rows,)), (logprob, "logprob", torch.float32, (rows,)),
+                                (entropy, "entropy", torch.float32, (rows,)),
+                                (top_ids, "top_ids", torch.int32, (rows, top)),
+                                (top_logprobs, "top_logprobs", torch.float32, (rows, top))):
+        if t is not None:
+            _expect(t, name, (typ,), shape)
+    need = int(lib().sr_token_logprobs_scratch(rows, vocab, top))
+    _call((logits, tokens, logprob, entropy, top_ids, top_logprobs), stream,
+          lambda s, w: lib().sr_token_logprobs(SR_F32 if logits.dtype == torch.float32 else SR_BF16, _ptr(logits),
+                                               stride, rows, vocab, temperature, _ptr(tokens), top, _ptr(logprob),
+                                               _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), w, need, s),
+          need, torch.float32)

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <cstdio>
+#include <exception>
 #include <string>
 
 typedef uint16_t bf16_t;  // bf16 bit pattern
@@ -102,7 +103,26 @@ struct Error {
   int status;
   std::string msg;
 };
-void set_error(const std::string& msg);
+void set_last_error(const char* msg);   // the calling thread's message for sr_last_error (empty clears it)
+
+// Runs a C entry point: no exception leaves it, and its message is kept.
+template <typename F>
+inline int guarded(F&& f) noexcept {
+  try {
+    f();
+    set_last_error("");
+    return 0;
+  } catch (const Error& e) {
+    set_last_error(e.msg.c_str());
+    return e.status;
+  } catch (const std::exception& e) {
+    set_last_error((std::string("internal error: ") + e.what()).c_str());
+    return 5;
+  } catch (...) {
+    set_last_error("internal error");
+    return 5;
+  }
+}
 }  // namespace sr
 
 #define SR_HIP(call)                                                                  \

@@ -1033,20 +1033,7 @@ static void reward_entry(const sr_model* gen, const sr_model* rm, const int32_t*
 
 template <typename F>
 static sr_status guard(F&& f) {
-  try {
-    f();
-    t_err.clear();
-    return SR_OK;
-  } catch (const Error& e) {
-    t_err = e.msg;
-    return (sr_status)e.status;
-  } catch (const std::exception& e) {
-    t_err = std::string("internal error: ") + e.what();
-    return SR_ERR_INTERNAL;
-  } catch (...) {
-    t_err = "internal error";
-    return SR_ERR_INTERNAL;
-  }
+  return (sr_status)guarded(f);
 }
 
 void set_last_error(const char* msg) { t_err = msg; }

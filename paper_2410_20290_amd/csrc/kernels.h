@@ -201,6 +201,89 @@ struct CompactArgs {
   int32_t* new_count;        // [1] written when keep_flag is given
 };
 void compact(const CompactArgs& a, hipStream_t s);
+// ---- the paged cache (see specrej_ops.h; lengths and ids are clamped or
+// checked where they are read) ----------------------------------------------
+struct PageForkArgs {
+  const int32_t *table, *lens;
+  int rows, max_pages;
+  const int32_t* parent;
+  int new_rows, shift, n_pages, window, sinks;   // shift = log2(page_tokens)
+  int32_t *table_out, *lens_out, *refs_out;
+};
+void page_fork(const PageForkArgs& a, hipStream_t s);
+
+struct PagePool {
+  void* pool;
+  int64_t block_bytes;
+  int n_layers, hkv, row_bytes, shift, n_pages;   // row_bytes: one key of one head
+};
+struct PageReserveArgs {
+  PagePool p;
+  const int32_t *table, *lens, *refs;
+  int rows, max_pages;
+  const int32_t* n_add;
+  int n_add_all;
+  int32_t *table_out, *lens_out, *refs_out, *granted, *info, *scratch;
+};
+size_t page_reserve_scratch(int rows, int max_pages, int n_pages);
+void page_reserve(const PageReserveArgs& a, hipStream_t s);
+
+struct PageCompactArgs {
+  PagePool p;
+  const int32_t *table, *lens, *refs;
+  int rows, max_pages;
+  int32_t *table_out, *refs_out, *info, *scratch;
+};
+size_t page_compact_scratch(int n_pages);
+void page_compact(const PageCompactArgs& a, hipStream_t s);
+
+struct PageAppendArgs {
+  int dtype, hd, hq, hkv, rows, lr;
+  const float* qkv;
+  const double* freqs;
+  int rot;
+  bool interleaved;
+  void *kpool, *vpool;
+  int shift, n_pages;
+  const int32_t* table;
+  int max_pages;
+  const int32_t *lens, *n_new;
+  float* q;
+};
+void page_append(const PageAppendArgs& a, hipStream_t s);
+
+struct PagedAttnArgs {
+  int dtype, hd, hq, hkv, rows, lr;
+  const float* q;
+  const void *kpool, *vpool;
+  int shift, n_pages;
+  const int32_t* table;
+  int max_pages;
+  const int32_t *lens, *n_new;
+  int window, sinks, shared, max_len;
+  void* out;
+  float* part;   // paged_attn_scratch() floats
+};
+size_t paged_attn_scratch(const PagedAttnArgs& a);
+void paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+// ---- log-probabilities of given tokens (see specrej_ops.h) -------------------
+struct LogprobArgs {
+  int dtype;
+  const void* logits;
+  int64_t row_stride;
+  int rows, vocab;
+  float temperature;
+  const int32_t* tokens;
+  int top;
+  float *logprob, *entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+  float* scratch;
+};
+size_t token_logprobs_scratch(int rows, int vocab, int top);
+void token_logprobs(const LogprobArgs& a, hipStream_t s);
+
 // best[0] = index of the best entry of (score, cand) pairs, n >= 1.
 void argmax_best(const float* score, const int32_t* cand, const int32_t* n_dev, int n_max,
                  int32_t* best, hipStream_t s);
