@@ -172,7 +172,7 @@ size_t sr_paged_attention_scratch(int32_t dtype, int32_t head_dim, int32_t n_hea
 /* Log-probabilities under softmax(logits[r] / temperature), the distribution
  * sr_sample draws from (temperature > 0), for every row r < rows of logits
  * (DEVICE dtype [rows][row_stride], vocab <= row_stride entries used, vocab <=
- * 262144).  Any output may be NULL:
+ * 262144, rows <= 2^20).  Any output may be NULL:
  *   logprob[r] = ln p(tokens[r]) (tokens: DEVICE int32 [rows]; -1, padding: 0;
  *                any other value outside [0, vocab): NaN),
  *   entropy[r] = - sum_i p_i ln p_i (nats),

@@ -309,11 +309,12 @@ sr_status sr_token_logprobs(int32_t dtype, const void* logits, int64_t row_strid
     require(dtype == SR_F32 || dtype == SR_BF16, "unknown dtype");
     require(rows >= 0 && vocab >= 1 && row_stride >= vocab, "bad rows / vocab / row_stride");
     require(std::isfinite(temperature) && temperature > 0.f, "temperature must be finite and > 0");
-    require(std::isfinite((float)(1.0 / (double)temperature)), "temperature too small");
+    require(std::isfinite((float)(1.5 / (double)temperature)), "temperature too small");
     require(top >= 0 && top <= vocab, "top must be in [0, vocab]");
     supported(vocab <= 262144, "vocab above 262144");
     supported(top <= 32, "top above 32");
     supported(row_stride <= (int64_t)1 << 40, "row_stride above 2^40");
+    supported(rows <= 1 << 20, "at most 2^20 rows");
     if (rows == 0) return;
     require(logits && (!logprob || tokens), "NULL buffer");
     const int es = dtype == SR_BF16 ? 2 : 4;

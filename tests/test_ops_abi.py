@@ -152,7 +152,8 @@ LOGP = dict(dtype=sr.SR_F32, logits=0x100000, stride=1000, rows=2, vocab=1000, T
     (dict(T=1e-39), INVALID), (dict(top=-1), INVALID), (dict(top=33), UNSUPPORTED), (dict(vocab=3, top=4), INVALID),
     (dict(vocab=262145, stride=262145), UNSUPPORTED), (dict(logits=None), INVALID), (dict(tokens=None), INVALID),
     (dict(logits=0x100002), INVALID), (dict(lp=0x100000), INVALID), (dict(h=0x300004), INVALID),
-    (dict(tl=0x500000), INVALID)])
+    (dict(tl=0x500000), INVALID), (dict(rows=1, vocab=128256, stride=128256, n=3), SMALL),
+    (dict(rows=1, vocab=128256, stride=128256, scratch=None), SMALL), (dict(rows=(1 << 20) + 1), UNSUPPORTED)])
 def test_logprobs_refuse(L, kw, status):
     assert L.sr_token_logprobs(*args(LOGP, LOGP, kw)) == status and sr.last_error()
 
