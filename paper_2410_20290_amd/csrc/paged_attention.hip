@@ -1,6 +1,8 @@
 // Attention over the paged candidate cache: causal, with a sliding window and
 // sink tokens, rows of their own lengths.
 //
+//   paged_wave_kernel    (bf16, up to 16 query columns a row and KV head: single
+//                        tokens, short drafts): the waves split a row's keys
 //   paged_vector_kernel  (fp32, head_dim 32): one token and a few query heads
 //                        of a KV head per work-group, vector ALU
 //   paged_merge_kernel   joins the partials of a token's work-groups
@@ -11,14 +13,14 @@
 // where there is one slot.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
+#include "attn_tiles.h"
 #include "common.h"
 #include "kernels.h"
 #include "paged.h"
 
 namespace sr {
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // A row's length, the call's tokens in it, and the first of their positions.
 struct RowState {
@@ -174,6 +176,271 @@ __global__ void __launch_bounds__(256) paged_vector_kernel(PagedAttnArgs a, int 
   }
 }
 
+// ------------------------------------------------------- waves split keys
+// What the 16 keys of an entry that names no page, or that nobody sees, are
+// read from: their scores are masked, and 0 times a finite value stays 0.
+static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
+
+// bf16, head_dim 64 or 128, at most 16 query columns: column x is token x / G of
+// the row's, query head x % G of the KV head's G, so the columns' queries and
+// outputs are contiguous.  Work-group = (split, KV head, row), NW waves; every
+// wave takes an even share of the 32-key blocks that hold visible keys and waits
+// on no other until the merge.
+//   S^T = K Q^T   (v_mfma_f32_16x16x32_bf16): the A operand, 16 keys x 32 dims,
+//         comes from memory straight into registers.
+//   O^T += V^T P^T: a V block goes memory -> LDS (the wave's own double buffer)
+//         and its A operand comes from two transpose reads; the contraction
+//         visits the keys in the order the lane holds their probabilities.
+// The next block's keys and values are in flight while one is computed.  A
+// block's 16-key halves lie in one page each; lane i holds the page numbers of
+// block i of a run of 64, so a block's addresses cost two lane reads.  Lanes
+// whose key nobody sees read a visible key of the half instead (KeyBlocks::safe).
+// Bound by memory: each key and value byte is read once.
+template <int HD, int NW>
+__global__ void __launch_bounds__(64 * NW)
+paged_wave_kernel(PagedAttnArgs a, int splits, float qscale) {
+  constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
+  constexpr int KPD = 64 / CPK, NV = 32 / KPD;     // keys per V copy, copies of a block
+  constexpr int INFLIGHT = 2 * KS + NV;            // memory operations of a block
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[NW * 2 * VB];
+  const int split = blockIdx.x, h = blockIdx.y, row = blockIdx.z;
+  const RowState rs = row_state(a, row);
+  if (rs.n == 0) return;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fg = lane >> 4;
+  const int g = a.hq / a.hkv, t = fr / g;          // this lane's column
+  const bool live = t < rs.n;
+  const int end_c = rs.p0 + (live ? t : 0) + 1, lo_c = window_start(end_c - 1, a.window);
+  const int lo_last = window_start(rs.len - 1, a.window);
+  KeyBlocks kb;
+  kb.set(0, a.sinks, window_start(rs.p0, a.window), rs.len);
+  const int shares = splits * NW, me = split * NW + wave;
+  const int i0 = (int)((int64_t)kb.count * me / shares), i1 = (int)((int64_t)kb.count * (me + 1) / shares);
+  const int32_t* tab = a.table + (int64_t)row * a.max_pages;
+  bf16_t* vbuf = lds + wave * 2 * VB;
+
+  // The pages of blocks [base, base + 64) of this wave, -1 for none.
+  int base = i0, d0 = -1, d1 = -1;
+  auto look_up = [&] {
+    d0 = d1 = -1;
+    if (base + lane < i1) {
+      const int k0 = kb.key0(base + lane);
+      const int p0 = kb.any16(k0) ? tab[k0 >> a.shift] : -1;
+      const int p1 = kb.any16(k0 + 16) ? tab[(k0 + 16) >> a.shift] : -1;
+      d0 = (uint32_t)p0 < (uint32_t)a.n_pages ? p0 : -1;
+      d1 = (uint32_t)p1 < (uint32_t)a.n_pages ? p1 : -1;
+    }
+  };
+  auto at = [&](const void* pool, int page, int key) -> const bf16_t* {
+    return page < 0 ? zero_keys : (const bf16_t*)pool + page_offset(page, a.hkv, h, a.shift, key, HD);
+  };
+  auto halves = [&](int b, int (&pg)[2]) {
+    pg[0] = __builtin_amdgcn_readlane(d0, b);
+    pg[1] = __builtin_amdgcn_readlane(d1, b);
+  };
+  auto load_block = [&](int b, uint4 (&kr)[2][KS], int buf) {
+    int pg[2];
+    halves(b, pg);
+    const int k0 = kb.key0(base + b);
+    const bool whole = kb.all32(k0);
+    int j[2] = {fr, fr};
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (pg[u] >= 0) j[u] = kb.safe(k0 + 16 * u, k0 + 16 * u + fr) - (k0 + 16 * u);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16_t* src = at(a.kpool, pg[u], k0 + 16 * u);
+#pragma unroll
+      for (int st = 0; st < KS; ++st)
+        kr[u][st] = *reinterpret_cast<const uint4*>(src + (j[u] * HD + 8 * fg + 32 * st));
+    }
+    const BufRsrc rv[2] = {buf_rsrc(at(a.vpool, pg[0], k0)), buf_rsrc(at(a.vpool, pg[1], k0 + 16))};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int u = i * KPD / 16, kk = i * KPD + lane / CPK;   // half, key of the block
+      int jj = kk - 16 * u;
+      if (!whole && pg[u] >= 0) jj = kb.safe(k0 + 16 * u, k0 + kk) - (k0 + 16 * u);
+      dma16(rv[u], (uint32_t)((jj * HD + 8 * vslot<CPK>(kk, lane % CPK)) * 2), 0, vbuf + buf * VB + i * 512);
+    }
+  };
+
+  // The first block's loads go out before the queries are read.
+  uint4 ka[2][KS], kc[2][KS];
+  look_up();
+  if (i0 < i1) load_block(0, ka, 0);
+
+  // Q^T fragments (B operand): lane holds Q[column fr][32 s + 8 fg .. + 8]
+  bf16x8 qf[KS];
+  {
+    const float* qr = a.q + (((int64_t)row * a.lr + (live ? t : 0)) * a.hq + h * g + (live ? fr - t * g : 0)) * HD;
+#pragma unroll
+    for (int st = 0; st < KS; ++st) {
+      const float4 x = *reinterpret_cast<const float4*>(qr + 32 * st + 8 * fg);
+      const float4 y = *reinterpret_cast<const float4*>(qr + 32 * st + 8 * fg + 4);
+      const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[st][e] = (__bf16)(v[e] * qscale);
+    }
+  }
+
+  f32x4 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  // transpose-read addresses: lane names 4 dims (dt 16 + 4 (fr & 3) ..) of key
+  // 4 fg + (fr >> 2), and of the key 16 on (16 rows on, same slots)
+  uint32_t vaddr[DT];
+  {
+    const int kr0 = 4 * fg + (fr >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      vaddr[dt] = lds_addr(vbuf + kr0 * HD + 8 * vslot<CPK>(kr0, 2 * dt + ((fr & 3) >> 1)) + 4 * (fr & 1));
+  }
+  auto compute = [&](int b, const uint4 (&kr)[2][KS], auto bufc) {
+    f32x4 st[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      st[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s2 = 0; s2 < KS; ++s2)
+        st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[u][s2]), qf[s2], st[u], 0, 0, 0);
+    }
+    const int k0 = kb.key0(base + b);
+    int pg[2];
+    halves(b, pg);
+    float sv[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sv[i] = st[0][i];
+      sv[4 + i] = st[1][i];
+    }
+    // (uniform) some column does not see some key of the block
+    if (k0 + 32 > rs.p0 + 1 || (k0 < lo_last && k0 + 32 > a.sinks) || pg[0] < 0 || pg[1] < 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int j = k0 + 4 * fg + (i & 3) + 16 * (i >> 2);
+        const bool sees = j < end_c && (j >= lo_c || j < a.sinks) && pg[i >> 2] >= 0;
+        if (!sees) sv[i] = -INFINITY;
+      }
+    }
+    float mt = sv[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mt = fmaxf(mt, sv[i]);
+    mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+    mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+    // rescaled only when some column's maximum grows; the exact maximum, so that
+    // the largest probability, 1, loses nothing in bf16
+    if (__any(mt > m)) {
+      const float mn = fmaxf(m, mt);
+      const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= corr;
+      m = mn;
+    }
+    const float mr = m == -INFINITY ? 0.f : m;   // (a column without a key so far)
+    bf16x8 pf;
+    float ps = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float pv = __builtin_amdgcn_exp2f(sv[i] - mr);
+      ps += pv;
+      pf[i] = (__bf16)pv;
+    }
+    l += ps;
+    constexpr int BUF = decltype(bufc)::value;
+#pragma unroll
+    for (int e0 = 0; e0 < DT; e0 += 4) {
+      const uint32_t va[4] = {vaddr[e0], vaddr[e0 + 1], vaddr[e0 + 2], vaddr[e0 + 3]};
+      i16x4 lo[4], hi[4];
+      lds_read_tr16_pairs<4, BUF * VB * 2, (BUF * VB + 16 * HD) * 2>(va, lo, hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        o[e0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tr16_pair(lo[i], hi[i]), pf, o[e0 + i], 0, 0, 0);
+    }
+  };
+
+  // One block ahead.  Every fetch in the loop is unconditional, so the
+  // compiler's own waits count the younger block's loads as in flight.
+  const std::integral_constant<int, 0> buf0{};
+  const std::integral_constant<int, 1> buf1{};
+  const std::integral_constant<int, INFLIGHT> next{};
+  auto compute_after = [&](auto left, int b, const uint4 (&kr)[2][KS], auto bufc) {
+    __builtin_amdgcn_sched_barrier(0);   // (the fetch before it stays before it)
+    vm_wait<decltype(left)::value>();
+    compute(b, kr, bufc);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  while (base < i1) {
+    const int nb = imin(64, i1 - base);
+    int b = 0;
+    for (; b + 2 < nb; b += 2) {
+      load_block(b + 1, kc, 1);
+      compute_after(next, b, ka, buf0);
+      load_block(b + 2, ka, 0);
+      compute_after(next, b + 1, kc, buf1);
+    }
+    if (b + 1 < nb) {
+      load_block(b + 1, kc, 1);
+      compute_after(next, b, ka, buf0);
+      compute_after(buf0, b + 1, kc, buf1);
+    } else {
+      compute_after(buf0, b, ka, buf0);
+    }
+    base += 64;
+    if (base < i1) {   // (a run of 64 blocks drains: one round trip in 2048 keys)
+      look_up();
+      load_block(0, ka, 0);
+    }
+  }
+
+  // join the waves: per column (max, sum, unnormalised output)
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  __syncthreads();
+  float* sm = reinterpret_cast<float*>(lds);   // [NW][16][HD + 2]
+  float* w = sm + (wave * 16 + fr) * (HD + 2);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[dt * 16 + 4 * fg + i] = o[dt][i];
+  if (fg == 0) {
+    w[HD] = m;
+    w[HD + 1] = l;
+  }
+  __syncthreads();
+  const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, splits};
+  for (int i = threadIdx.x; i < rs.n * g * HD; i += 64 * NW) {
+    const int x = i / HD, d = i % HD;
+    float M = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) M = fmaxf(M, sm[(k * 16 + x) * (HD + 2) + HD]);
+    float L = 0.f, A = 0.f;
+    if (M != -INFINITY) {
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        const float* ws = sm + (k * 16 + x) * (HD + 2);
+        const float c = __builtin_amdgcn_exp2f(ws[HD] - M);
+        L += ws[HD + 1] * c;
+        A += ws[d] * c;
+      }
+    }
+    const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
+    if (splits == 1) {
+      ((bf16_t*)a.out)[th * HD + d] = f32_to_bf16(L > 0.f ? A / L : 0.f);
+    } else {
+      pt.o(th, split, HD)[d] = A;
+      if (d == 0) {
+        pt.ml(th, split, HD)[0] = M;
+        pt.ml(th, split, HD)[1] = L;
+      }
+    }
+  }
+}
+
 // ----------------------------------------------------------------- merge
 // A wave joins the slots of one (token, query head).
 template <typename T, int HD>
@@ -200,19 +467,40 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
 }
 
 // ------------------------------------------------------------------ plan
+enum PagedKind { PAGED_VECTOR, PAGED_WAVE };
 struct PagedPlan {
-  int slots;
+  PagedKind kind;
+  int nw;      // PAGED_WAVE: waves of a work-group
+  int slots;   // partial slots (1: the pass writes the output)
 };
 
 // Query heads of a work-group of the vector kernel.
 static int vector_heads(int g) { return g % 4 == 0 ? 4 : g % 2 == 0 ? 2 : 1; }
 
+// Keys that a row's queries see at most, as far as the host knows.
+static int64_t planned_keys(const PagedAttnArgs& a) {
+  int64_t keys = std::min<int64_t>(a.max_len, (int64_t)a.max_pages << a.shift);
+  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + a.lr + a.sinks);
+  return keys;
+}
+
+constexpr int kWaveTarget = 2048;
 static PagedPlan paged_plan(const PagedAttnArgs& a) {
   PagedPlan p;
-  const int64_t cap = (int64_t)a.max_pages << a.shift;
-  int64_t keys = std::min<int64_t>(a.max_len, cap);
-  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks);
-  const int64_t groups = (int64_t)a.rows * a.lr * (a.hq / vector_heads(a.hq / a.hkv));
+  const int g = a.hq / a.hkv;
+  const int64_t keys = planned_keys(a);
+  p.nw = 1;
+  if (a.dtype == SR_BF16 && a.hd >= 64 && a.lr * g <= 16) {
+    p.kind = PAGED_WAVE;
+    const int64_t pairs = (int64_t)a.rows * a.hkv, blocks = (keys + 31) / 32;
+    int64_t want = std::max<int64_t>(1, std::min<int64_t>(kWaveTarget / pairs, blocks / 2));
+    if (want > 8 && pairs * 8 >= 1024) want = 8;
+    p.nw = want >= 8 ? 8 : want >= 4 ? 4 : want >= 2 ? 2 : 1;
+    p.slots = (int)std::min<int64_t>(64, (want + p.nw - 1) / p.nw);
+    return p;
+  }
+  p.kind = PAGED_VECTOR;
+  const int64_t groups = (int64_t)a.rows * a.lr * (a.hq / vector_heads(g));
   p.slots = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, keys / 256, 64}));
   return p;
 }
@@ -231,8 +519,7 @@ static void launch_merge(const PagedAttnArgs& a, int slots, hipStream_t s) {
 }
 
 template <typename T, int HD>
-static void launch_vector(const PagedAttnArgs& a, hipStream_t s) {
-  const PagedPlan p = paged_plan(a);
+static void launch_vector(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
   const int gc = vector_heads(a.hq / a.hkv);
   const dim3 grid((unsigned)((int64_t)a.rows * a.lr * p.slots), a.hq / gc);
@@ -246,18 +533,38 @@ static void launch_vector(const PagedAttnArgs& a, hipStream_t s) {
 }
 
 template <typename T>
-static void vector_by_hd(const PagedAttnArgs& a, hipStream_t s) {
+static void vector_by_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   switch (a.hd) {
-    case 32: launch_vector<T, 32>(a, s); break;
-    case 64: launch_vector<T, 64>(a, s); break;
-    default: launch_vector<T, 128>(a, s); break;
+    case 32: launch_vector<T, 32>(a, p, s); break;
+    case 64: launch_vector<T, 64>(a, p, s); break;
+    default: launch_vector<T, 128>(a, p, s); break;
   }
+}
+
+template <int HD>
+static void launch_wave(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
+  const float qscale = kLog2e / sqrtf((float)HD);
+  const dim3 grid(p.slots, a.hkv, a.rows);
+  switch (p.nw) {
+    case 8: SR_LAUNCH((paged_wave_kernel<HD, 8>), grid, dim3(512), 0, s, a, p.slots, qscale); break;
+    case 4: SR_LAUNCH((paged_wave_kernel<HD, 4>), grid, dim3(256), 0, s, a, p.slots, qscale); break;
+    case 2: SR_LAUNCH((paged_wave_kernel<HD, 2>), grid, dim3(128), 0, s, a, p.slots, qscale); break;
+    default: SR_LAUNCH((paged_wave_kernel<HD, 1>), grid, dim3(64), 0, s, a, p.slots, qscale); break;
+  }
+  SR_CHECK_LAUNCH();
+  if (p.slots > 1) launch_merge<bf16_t, HD>(a, p.slots, s);
 }
 
 void paged_attn(const PagedAttnArgs& a, hipStream_t s) {
   if (a.rows <= 0 || a.lr <= 0) return;
-  if (a.dtype == SR_BF16) vector_by_hd<bf16_t>(a, s);
-  else vector_by_hd<float>(a, s);
+  const PagedPlan p = paged_plan(a);
+  if (p.kind == PAGED_WAVE) {
+    if (a.hd == 128) launch_wave<128>(a, p, s);
+    else launch_wave<64>(a, p, s);
+    return;
+  }
+  if (a.dtype == SR_BF16) vector_by_hd<bf16_t>(a, p, s);
+  else vector_by_hd<float>(a, p, s);
 }
 
 }  // namespace sr
