@@ -3,6 +3,9 @@
 //
 //   paged_wave_kernel    (bf16, up to 16 query columns a row and KV head: single
 //                        tokens, short drafts): the waves split a row's keys
+//   paged_tile_kernel    (bf16): 128 query columns a work-group, keys staged in
+//                        LDS for all of them: prompts, and the part of the rows
+//                        that lies in the pages of row 0, once for all rows
 //   paged_vector_kernel  (fp32, head_dim 32): one token and a few query heads
 //                        of a KV head per work-group, vector ALU
 //   paged_merge_kernel   joins the partials of a token's work-groups
@@ -12,6 +15,7 @@
 // maximum and the sum in one of the `slots` partial slots, or the output itself
 // where there is one slot.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -193,12 +197,13 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 //         visits the keys in the order the lane holds their probabilities.
 // The next block's keys and values are in flight while one is computed.  A
 // block's 16-key halves lie in one page each; lane i holds the page numbers of
-// block i of a run of 64, so a block's addresses cost two lane reads.  Lanes
+// block i of a run of 64, so a block's addresses cost two lane reads.  The keys
+// below common[row] are another pass's.  Lanes
 // whose key nobody sees read a visible key of the half instead (KeyBlocks::safe).
 // Bound by memory: each key and value byte is read once.
 template <int HD, int NW>
 __global__ void __launch_bounds__(64 * NW)
-paged_wave_kernel(PagedAttnArgs a, int splits, float qscale) {
+paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slot0, int slots, float qscale) {
   constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
   constexpr int KPD = 64 / CPK, NV = 32 / KPD;     // keys per V copy, copies of a block
   constexpr int INFLIGHT = 2 * KS + NV;            // memory operations of a block
@@ -214,7 +219,7 @@ paged_wave_kernel(PagedAttnArgs a, int splits, float qscale) {
   const int end_c = rs.p0 + (live ? t : 0) + 1, lo_c = window_start(end_c - 1, a.window);
   const int lo_last = window_start(rs.len - 1, a.window);
   KeyBlocks kb;
-  kb.set(0, a.sinks, window_start(rs.p0, a.window), rs.len);
+  kb.set(common ? common[row] : 0, a.sinks, window_start(rs.p0, a.window), rs.len);
   const int shares = splits * NW, me = split * NW + wave;
   const int i0 = (int)((int64_t)kb.count * me / shares), i1 = (int)((int64_t)kb.count * (me + 1) / shares);
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
@@ -412,7 +417,7 @@ paged_wave_kernel(PagedAttnArgs a, int splits, float qscale) {
     w[HD + 1] = l;
   }
   __syncthreads();
-  const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, splits};
+  const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, slots};
   for (int i = threadIdx.x; i < rs.n * g * HD; i += 64 * NW) {
     const int x = i / HD, d = i % HD;
     float M = -INFINITY;
@@ -429,15 +434,414 @@ paged_wave_kernel(PagedAttnArgs a, int splits, float qscale) {
       }
     }
     const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
-    if (splits == 1) {
+    if (slots == 1) {
       ((bf16_t*)a.out)[th * HD + d] = f32_to_bf16(L > 0.f ? A / L : 0.f);
     } else {
-      pt.o(th, split, HD)[d] = A;
+      pt.o(th, slot0 + split, HD)[d] = A;
       if (d == 0) {
-        pt.ml(th, split, HD)[0] = M;
-        pt.ml(th, split, HD)[1] = L;
+        pt.ml(th, slot0 + split, HD)[0] = M;
+        pt.ml(th, slot0 + split, HD)[1] = L;
       }
     }
+  }
+}
+
+// -------------------------------------------------------- query tiles
+// The leading keys of every row that the tile kernel attends for all rows at
+// once: those in pages that the row has in common with row 0, before every
+// query of the row, a multiple of 32 up to `shared`; none once the window of the
+// row's first query has left key 0 (so a key that the pass reads is seen by some
+// query).  A wave per row.
+__global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int32_t* __restrict__ common) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= a.rows) return;
+  const RowState rs = row_state(a, row);
+  const int len0 = clamp_len(a.lens[0], a.max_pages, a.shift);
+  int c = rs.n > 0 && window_start(rs.p0, a.window) == 0 ? imin(imin(a.shared, rs.p0), len0) : 0;
+  const int32_t* mine = a.table + (int64_t)row * a.max_pages;
+  const int pages = (c + (1 << a.shift) - 1) >> a.shift;
+  for (int p = 0; p < pages; p += 64) {
+    const int q = p + lane;
+    const uint64_t other = __ballot(q < pages && mine[q] != a.table[q]);
+    if (other) {
+      c = imin(c, (p + (int)__builtin_ctzll(other)) << a.shift);
+      break;
+    }
+  }
+  if (lane == 0) common[row] = c & ~31;
+}
+
+// bf16 flash attention with v_mfma_f32_32x32x16_bf16, head_dim 64 or 128, 128
+// query columns a work-group, 32 a wave; column x is token x / G, query head x %
+// G of the KV head's G, so four query heads of eight tokens share a wave, and
+// the work-group's tokens are as few as they can be (their causal and window
+// edges cost the fewest masked keys).
+//   PRE = false: the tokens of one row, over all its keys.
+//   PRE = true:  the tokens of all rows, over row 0's leading keys; a column
+//                sees those its row has in common (`common`).
+//   S^T = K Q^T   (keys x columns): lane l holds, of every 32 keys, the 16 with
+//                 (key / 4) % 2 = l / 32 for column l % 32.
+//   O^T += V^T P^T: the contraction visits a 16-key chunk in the order the lane
+//                 holds it, so the B operand is the lane's own probabilities;
+//                 the A operand comes from V by two LDS transpose reads.
+// The 32-key blocks that hold a visible key go memory -> LDS by
+// global_load_lds, four stages deep, one barrier a block; the scores of the next
+// block are formed under the probabilities of this one; 16-byte chunks sit
+// XOR-swizzled in the LDS rows.  Two work-groups a CU.  With several splits a
+// work-group takes an even share of the blocks.
+constexpr int kTileStages = 4;
+constexpr int kTileCols = 128;
+
+template <int HD, bool PRE>
+__global__ void __launch_bounds__(256, 2)
+paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slot0, int slots,
+                  float qscale) {
+  constexpr int KT = 32, NW = 4;
+  constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
+  constexpr int TILE = KT * HD;                // bf16 elements of a K (or V) block
+  constexpr int RPI = 64 / CPK;                // keys per copy instruction (1 KB)
+  constexpr int DPW = KT / RPI / NW;           // copies per wave of a K (or V) block
+  constexpr int CPW = 2 * DPW;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[kTileStages * 2 * TILE];
+  __shared__ int bounds[NW][2];
+  // a 1-D grid dealt round-robin to the 8 XCDs: each takes consecutive logical
+  // blocks, the query tiles of one (row, KV head, split) fastest, the last and
+  // longest first, so that those reading the same keys share one L2
+  const int g = a.hq / a.hkv;
+  const int X = (PRE ? a.rows * a.lr : a.lr) * g;                 // columns
+  const int ngq = (X + kTileCols - 1) / kTileCols, total = ngq * splits * a.hkv * (PRE ? 1 : a.rows);
+  const int per_xcd = (total + 7) / 8;
+  const int pid = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (pid >= total) return;
+  const int qg = ngq - 1 - pid % ngq;
+  const int split = pid / ngq % splits;
+  const int h = pid / (ngq * splits) % a.hkv;
+  const int row = PRE ? 0 : pid / (ngq * splits * a.hkv);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fh = lane >> 5;
+  const int x0 = qg * kTileCols, xw = x0 + 32 * wave;             // first column, of the wave too
+  const int token0 = PRE ? 0 : row * a.lr;
+  const RowState rs = row_state(a, row);
+  if (!PRE && x0 >= rs.n * g) return;
+
+  // This lane's column sees keys [0, sinks) and [lo, end); the wave's columns
+  // all see a key below `all_end` at or past `all_lo`, none one at or past
+  // wend.  Columns that are no query (live = false) see everything: their
+  // results are dropped.
+  bool live;
+  int lo_c = 0, end_c = INT_MAX;
+  {
+    const int x = xw + fr, tok = x / g;
+    if (PRE) {
+      live = x < X;
+      const int r = live ? tok / a.lr : 0, t = tok - r * a.lr;
+      const RowState cs = row_state(a, r);
+      live = live && t < cs.n;
+      if (live) {
+        end_c = common[r];
+        lo_c = imin(end_c, window_start(cs.p0 + t, a.window));
+      }
+    } else {
+      live = x < rs.n * g;
+      if (live) {
+        end_c = rs.p0 + tok + 1;
+        lo_c = window_start(end_c - 1, a.window);
+      }
+    }
+  }
+  int all_end, all_lo, wend, wlo;   // over the wave's columns: min end, max lo, max end, min lo
+  if (PRE) {
+    all_end = end_c;
+    all_lo = lo_c;
+    wend = live ? end_c : 0;
+    wlo = live ? lo_c : INT_MAX;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      all_end = imin(all_end, __shfl_xor(all_end, o, 64));
+      all_lo = imax(all_lo, __shfl_xor(all_lo, o, 64));
+      wend = imax(wend, __shfl_xor(wend, o, 64));
+      wlo = imin(wlo, __shfl_xor(wlo, o, 64));
+    }
+    all_end = __builtin_amdgcn_readfirstlane(all_end);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    wend = __builtin_amdgcn_readfirstlane(wend);
+    wlo = __builtin_amdgcn_readfirstlane(wlo);
+  } else {
+    const int last = imin(xw + 31, rs.n * g - 1);
+    const bool any = xw < rs.n * g;
+    all_end = rs.p0 + xw / g + 1;
+    wend = any ? rs.p0 + last / g + 1 : 0;
+    all_lo = any ? window_start(wend - 1, a.window) : 0;
+    wlo = window_start(all_end - 1, a.window);
+  }
+  KeyBlocks kb;
+  if (PRE) {
+    if (lane == 0) {
+      bounds[wave][0] = wlo;
+      bounds[wave][1] = wend;
+    }
+    __syncthreads();
+    const int end = imax(imax(bounds[0][1], bounds[1][1]), imax(bounds[2][1], bounds[3][1]));
+    const int lo = imin(imin(bounds[0][0], bounds[1][0]), imin(bounds[2][0], bounds[3][0]));
+    kb.set(0, a.sinks, __builtin_amdgcn_readfirstlane(imin(lo, end)), __builtin_amdgcn_readfirstlane(end));
+  } else {
+    const int last = imin(x0 + kTileCols - 1, rs.n * g - 1);
+    kb.set(0, a.sinks, window_start(rs.p0 + x0 / g, a.window), rs.p0 + last / g + 1);
+  }
+  const int i0 = (int)((int64_t)kb.count * split / splits), i1 = (int)((int64_t)kb.count * (split + 1) / splits);
+  const int ntile = i1 - i0;
+
+  // The wave's 32 queries, 16 bytes per lane along whole rows (clamped rows;
+  // results of columns that are no query are dropped)
+  constexpr int LPR = HD / 4, RPQ = 64 / LPR, NQ = 32 / RPQ;   // lanes per query, queries per load, loads
+  float4 qv[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int x = imin(xw + RPQ * i + lane / LPR, X - 1), tok = x / g;
+    qv[i] = reinterpret_cast<const float4*>(
+        a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
+  }
+
+  // The pages of blocks [64 c, 64 c + 64) of this split: lane i holds block
+  // 64 c + i's two, -1 for none.
+  const int32_t* tab = a.table + (int64_t)row * a.max_pages;
+  int d0 = -1, d1 = -1;
+  auto look_up = [&](int first) {
+    d0 = d1 = -1;
+    if (first + lane < ntile) {
+      const int k0 = kb.key0(i0 + first + lane);
+      const int p0 = kb.any16(k0) ? tab[k0 >> a.shift] : -1;
+      const int p1 = kb.any16(k0 + 16) ? tab[(k0 + 16) >> a.shift] : -1;
+      d0 = (uint32_t)p0 < (uint32_t)a.n_pages ? p0 : -1;
+      d1 = (uint32_t)p1 < (uint32_t)a.n_pages ? p1 : -1;
+    }
+  };
+  // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
+  // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
+  // stored there.  A key nobody sees is replaced by one of its half that
+  // somebody does, a half without any by zeros.
+  auto vswz = [](int k) { return HD == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2; };
+  uint32_t gone = 0;   // two bits a stage: halves that no page holds
+  auto issue = [&](int tile) {
+    if ((tile & 63) == 0) look_up(tile);
+    const int buf = tile % kTileStages;
+    bf16_t* kd = lds + buf * 2 * TILE;
+    bf16_t* vd = kd + TILE;
+    const int pg[2] = {__builtin_amdgcn_readlane(d0, tile & 63), __builtin_amdgcn_readlane(d1, tile & 63)};
+    gone = (gone & ~(3u << (2 * buf))) | ((pg[0] < 0 ? 1u : 0u) | (pg[1] < 0 ? 2u : 0u)) << (2 * buf);
+    const int k0 = kb.key0(i0 + tile);
+    const bool whole = kb.all32(k0);
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) {
+      const int r0 = RPI * (wave + NW * i), u = r0 >> 4;
+      const int r = r0 + lane / CPK, sl = lane % CPK, page = u ? pg[1] : pg[0];
+      int j = r & 15;
+      if (!whole && page >= 0) j = kb.safe(k0 + 16 * u, k0 + r) - (k0 + 16 * u);
+      const int64_t at = page < 0 ? 0 : page_offset(page, a.hkv, h, a.shift, k0 + 16 * u, HD);
+      const bf16_t* ks = page < 0 ? zero_keys : (const bf16_t*)a.kpool + at;
+      const bf16_t* vs = page < 0 ? zero_keys : (const bf16_t*)a.vpool + at;
+      dma16(reinterpret_cast<const char*>(ks + (j * HD + 8 * (sl ^ (r & (CPK - 1))))), kd + r0 * HD);
+      dma16(reinterpret_cast<const char*>(vs + (j * HD + 8 * (sl ^ vswz(r)))), vd + r0 * HD);
+    }
+  };
+  auto wait_barrier = [](auto n) {
+    constexpr int N = decltype(n)::value;
+    if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (N == 2) asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (N == 4) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else static_assert(N < 0, "add this wait count");
+  };
+
+  // LDS element offsets: the K fragment of key fr (chunk 2 s + fh), and the
+  // four dims dt 32 + 16 (l / 16 % 2) + 4 (l % 4) .. of V key 4 fh + l % 16 / 4
+  bf16x8 qf[KS];
+  int koff[KS];
+  uint32_t vbase[DT];   // LDS bytes, in the first stage's V block
+#pragma unroll
+  for (int s = 0; s < KS; ++s) koff[s] = fr * HD + 8 * ((2 * s + fh) ^ (fr & (CPK - 1)));
+  {
+    const int vk = 4 * fh + ((lane & 15) >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      vbase[dt] = lds_addr(lds + TILE + vk * HD +
+                           8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vswz(vk)) + 4 * (lane & 1));
+  }
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  // from the lowest finite score: while a column has seen only -inf its
+  // probabilities are exp2(-inf) = 0, where -inf - -inf would be NaN
+  float m = -FLT_MAX, l = 0.f;
+
+  auto zero = [](f32x16& sc) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+  };
+  // The scores `sc` of block `tile` (keys from `key` on) are there; the scores
+  // of the next block (K rows at `kn`) are formed into `sn`.  Per 16-key chunk:
+  // the K fragments and V of the chunk are read under the O MFMAs of the chunk
+  // before, then every score MFMA runs beside a share of the chunk's
+  // probabilities.
+  constexpr int KC = KS / 2;     // score MFMAs of a chunk
+  auto step = [&](int tile, f32x16& sc, f32x16& sn) {
+    const int key = kb.key0(i0 + tile);
+    const bf16_t* kn = lds + ((tile + 1) % kTileStages) * 2 * TILE;
+    uint32_t va[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) va[dt] = vbase[dt] + (uint32_t)(tile % kTileStages) * (2 * TILE * 2);
+    bf16x8 kf[KC], pf;
+    i16x4 lo[DT], hi[DT];
+    auto read_k = [&](int c) {
+#pragma unroll
+      for (int s = 0; s < KC; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kn + koff[c * KC + s]);
+    };
+    auto scores = [&](int c) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[c * KC + s], sn, 0, 0, 0);
+#pragma unroll
+        for (int e = s * 8 / KC; e < (s + 1) * 8 / KC; ++e) {
+          const float p = __builtin_amdgcn_exp2f(sc[8 * c + e] - m);
+          l += p;
+          pf[e] = (__bf16)p;
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 8 / KC, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 8 / KC, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 12 / KC, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto output = [&] {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf, o[dt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    read_k(0);
+    lds_read_tr16_pairs<DT, 0, 8 * HD * 2>(va, lo, hi);
+    const uint32_t out = gone >> (2 * (tile % kTileStages)) & 3u;
+    if (key + 32 > all_end || (key < all_lo && key + 32 > a.sinks) || out) {   // (uniform) an edge
+      asm volatile("");                        // (a branch, not selects on every block)
+      const int e0 = end_c - key - 4 * fh, l0 = lo_c - key - 4 * fh, s0 = a.sinks - key - 4 * fh;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = 8 * (e >> 2) + (e & 3);
+        if (!(j < e0 && (j >= l0 || j < s0)) || (out >> (e >> 3) & 1u)) sc[e] = -INFINITY;
+      }
+    }
+    float mt = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    mt = fmaxf(mt, other_half(mt));
+    if (__any(mt > m)) {
+      const float mn = fmaxf(m, mt);
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= corr;
+      m = mn;
+    }
+    zero(sn);
+    scores(0);
+    read_k(1);
+    output();
+    lds_read_tr16_pairs<DT, 16 * HD * 2, 24 * HD * 2>(va, lo, hi);
+    scores(1);
+    output();
+  };
+  // Before block i: block i + 1 landed too (its first scores are formed under
+  // block i; only the copies of i + 2 may still fly), and every wave is done
+  // with block i - 1, whose buffer takes block i + 3.
+  auto sync = [&](int tile) {
+    if (tile + 2 < ntile) wait_barrier(std::integral_constant<int, CPW>{});
+    else wait_barrier(std::integral_constant<int, 0>{});
+    if (tile + kTileStages - 1 < ntile) issue(tile + kTileStages - 1);
+  };
+  bf16_t* const slice = lds + wave * 32 * HD;
+  if (ntile > 0) {
+    // Blocks 0 and 1 go out first; the scaled bf16 queries pass through the
+    // buffers of blocks 2 and 3 (a 32-row slice per wave, chunks placed like
+    // K's) into fragments: lane holds Q[column fr][16 s + 8 fh .. + 8].
+    issue(0);
+    if (ntile > 1) issue(1);
+    bf16_t* qs = slice + 2 * 2 * TILE;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
+      const bf16x4 v = {(__bf16)(qv[i].x * qscale), (__bf16)(qv[i].y * qscale), (__bf16)(qv[i].z * qscale),
+                        (__bf16)(qv[i].w * qscale)};
+      *reinterpret_cast<bf16x4*>(qs + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qs + koff[s]);
+    f32x16 sa, sb;
+    zero(sa);
+    wait_barrier(std::integral_constant<int, 0>{});   // blocks 0 and 1, and every wave's queries read
+    if (ntile > 2) issue(2);
+    if (ntile > 3) issue(3);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds + koff[s]);
+      sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sa, 0, 0, 0);
+    }
+    // two blocks a round; the scores formed past the last block are those of a
+    // stale buffer and never used
+    for (int tile = 0; tile < ntile; tile += 2) {
+      if (tile > 0) sync(tile);
+      if (kb.key0(i0 + tile) < wend) step(tile, sa, sb);   // else past this wave's last query
+      if (tile + 1 < ntile) {
+        sync(tile + 1);
+        if (kb.key0(i0 + tile + 1) < wend) step(tile + 1, sb, sa);
+      }
+    }
+  }
+  l += other_half(l);
+  if (slots > 1) {
+    if (!live) return;
+    const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, slots};
+    const int x = xw + fr, tok = x / g;
+    const int64_t th = (int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g);
+    float* po = pt.o(th, slot0 + split, HD);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4*>(po + 32 * dt + 8 * q4 + 4 * fh) =
+            make_float4(o[dt][4 * q4], o[dt][4 * q4 + 1], o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
+    if (fh == 0) {
+      float* ml = pt.ml(th, slot0 + split, HD);
+      ml[0] = m;
+      ml[1] = l;
+    }
+    return;
+  }
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  wait_barrier(std::integral_constant<int, 0>{});   // every wave is done with the blocks
+  // The outputs pass through the wave's slice of LDS (chunks placed like K's),
+  // so that a query's leave as one contiguous run.
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const bf16x4 v = {(__bf16)(o[dt][4 * q4] * inv), (__bf16)(o[dt][4 * q4 + 1] * inv),
+                        (__bf16)(o[dt][4 * q4 + 2] * inv), (__bf16)(o[dt][4 * q4 + 3] * inv)};
+      *reinterpret_cast<bf16x4*>(slice + fr * HD + 8 * ((4 * dt + q4) ^ (fr & (CPK - 1))) + 4 * fh) = v;
+    }
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = RPI * i + lane / CPK, c = lane % CPK, x = xw + r, tok = x / g;
+    const uint4 v = *reinterpret_cast<const uint4*>(slice + r * HD + 8 * (c ^ (r & (CPK - 1))));
+    if (x >= rs.n * g) continue;
+    *reinterpret_cast<uint4*>((bf16_t*)a.out + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD + 8 * c) = v;
   }
 }
 
@@ -467,11 +871,13 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
 }
 
 // ------------------------------------------------------------------ plan
-enum PagedKind { PAGED_VECTOR, PAGED_WAVE };
+enum PagedKind { PAGED_VECTOR, PAGED_WAVE, PAGED_TILE };
 struct PagedPlan {
   PagedKind kind;
-  int nw;      // PAGED_WAVE: waves of a work-group
-  int slots;   // partial slots (1: the pass writes the output)
+  int nw;       // PAGED_WAVE: waves of a work-group
+  int splits;   // work-groups that share a row's keys
+  int pre;      // PAGED_WAVE: splits of the shared keys' own pass (0: none)
+  int slots() const { return splits + pre; }   // partial slots (1: the pass writes the output)
 };
 
 // Query heads of a work-group of the vector kernel.
@@ -484,31 +890,58 @@ static int64_t planned_keys(const PagedAttnArgs& a) {
   return keys;
 }
 
+// Work-groups of the tile kernel that fill the chip: two a CU.
+constexpr int kTileTarget = 512;
+constexpr int kMaxSplits = 64;
+
+// Splits of `blocks` 32-key blocks over work-groups of the tile kernel of which
+// `groups` take all keys, at least eight blocks each.
+static int tile_splits(int64_t groups, int64_t blocks) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kTileTarget / groups, blocks / 8, kMaxSplits}));
+}
+
+// Waves that fill the chip.
 constexpr int kWaveTarget = 2048;
+// From here on rows and shared keys the shared part has a pass of its own.
+constexpr int kShareMinRows = 8, kShareMinKeys = 128;
+
 static PagedPlan paged_plan(const PagedAttnArgs& a) {
-  PagedPlan p;
+  PagedPlan p{PAGED_VECTOR, 1, 1, 0};
   const int g = a.hq / a.hkv;
-  const int64_t keys = planned_keys(a);
-  p.nw = 1;
+  int64_t keys = planned_keys(a);
   if (a.dtype == SR_BF16 && a.hd >= 64 && a.lr * g <= 16) {
     p.kind = PAGED_WAVE;
+    const bool far = a.window > 0 && a.max_len > a.window;   // (windows have left key 0)
+    const int64_t shared = far ? 0 : std::min<int64_t>(a.shared, keys - a.lr);
+    if (a.rows >= kShareMinRows && shared >= kShareMinKeys) {
+      const int64_t tiles = ((int64_t)a.rows * a.lr * g + kTileCols - 1) / kTileCols;
+      p.pre = tile_splits(tiles * a.hkv, shared / 32);
+      keys -= shared;
+    }
     const int64_t pairs = (int64_t)a.rows * a.hkv, blocks = (keys + 31) / 32;
     int64_t want = std::max<int64_t>(1, std::min<int64_t>(kWaveTarget / pairs, blocks / 2));
     if (want > 8 && pairs * 8 >= 1024) want = 8;
     p.nw = want >= 8 ? 8 : want >= 4 ? 4 : want >= 2 ? 2 : 1;
-    p.slots = (int)std::min<int64_t>(64, (want + p.nw - 1) / p.nw);
-    return p;
+    p.splits = (int)std::min<int64_t>(kMaxSplits, (want + p.nw - 1) / p.nw);
+  } else if (a.dtype == SR_BF16 && a.hd >= 64) {
+    p.kind = PAGED_TILE;
+    const int64_t tiles = ((int64_t)a.lr * g + kTileCols - 1) / kTileCols;
+    p.splits = tile_splits(tiles * a.hkv * a.rows, keys / 32);
+  } else {
+    const int64_t groups = (int64_t)a.rows * a.lr * (a.hq / vector_heads(g));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, keys / 256, kMaxSplits}));
   }
-  p.kind = PAGED_VECTOR;
-  const int64_t groups = (int64_t)a.rows * a.lr * (a.hq / vector_heads(g));
-  p.slots = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, keys / 256, 64}));
   return p;
 }
 
+// Scratch: the partial slots, then common[rows].
+static size_t partial_floats(const PagedAttnArgs& a, const PagedPlan& p) {
+  return p.slots() > 1 ? (size_t)a.rows * a.lr * a.hq * p.slots() * (a.hd + 2) : 0;
+}
 size_t paged_attn_scratch(const PagedAttnArgs& a) {
   if (a.rows <= 0 || a.lr <= 0) return 0;
   const PagedPlan p = paged_plan(a);
-  return p.slots > 1 ? (size_t)a.rows * a.lr * a.hq * p.slots * (a.hd + 2) : 0;
+  return partial_floats(a, p) + (p.pre ? a.rows : 0);
 }
 
 template <typename T, int HD>
@@ -522,14 +955,14 @@ template <typename T, int HD>
 static void launch_vector(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
   const int gc = vector_heads(a.hq / a.hkv);
-  const dim3 grid((unsigned)((int64_t)a.rows * a.lr * p.slots), a.hq / gc);
+  const dim3 grid((unsigned)((int64_t)a.rows * a.lr * p.splits), a.hq / gc);
   switch (gc) {
-    case 4: SR_LAUNCH((paged_vector_kernel<T, HD, 4>), grid, dim3(256), 0, s, a, p.slots, qscale); break;
-    case 2: SR_LAUNCH((paged_vector_kernel<T, HD, 2>), grid, dim3(256), 0, s, a, p.slots, qscale); break;
-    default: SR_LAUNCH((paged_vector_kernel<T, HD, 1>), grid, dim3(256), 0, s, a, p.slots, qscale); break;
+    case 4: SR_LAUNCH((paged_vector_kernel<T, HD, 4>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
+    case 2: SR_LAUNCH((paged_vector_kernel<T, HD, 2>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
+    default: SR_LAUNCH((paged_vector_kernel<T, HD, 1>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
   }
   SR_CHECK_LAUNCH();
-  if (p.slots > 1) launch_merge<T, HD>(a, p.slots, s);
+  if (p.splits > 1) launch_merge<T, HD>(a, p.splits, s);
 }
 
 template <typename T>
@@ -541,26 +974,58 @@ static void vector_by_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t
   }
 }
 
+template <int HD, bool PRE>
+static void launch_tile(const PagedAttnArgs& a, const int32_t* common, int splits, int slots, hipStream_t s) {
+  const float qscale = kLog2e / sqrtf((float)HD);
+  const int64_t cols = (int64_t)(PRE ? a.rows : 1) * a.lr * (a.hq / a.hkv);
+  const int64_t total = (cols + kTileCols - 1) / kTileCols * splits * a.hkv * (PRE ? 1 : a.rows);
+  SR_REQUIRE(total <= (int64_t)INT_MAX - 8, SR_ERR_UNSUPPORTED, "attention grid too large");
+  SR_LAUNCH((paged_tile_kernel<HD, PRE>), dim3((unsigned)(8 * ((total + 7) / 8))), dim3(256), 0, s, a, common, splits, 0,
+            slots, qscale);
+  SR_CHECK_LAUNCH();
+}
+
 template <int HD>
 static void launch_wave(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
-  const dim3 grid(p.slots, a.hkv, a.rows);
-  switch (p.nw) {
-    case 8: SR_LAUNCH((paged_wave_kernel<HD, 8>), grid, dim3(512), 0, s, a, p.slots, qscale); break;
-    case 4: SR_LAUNCH((paged_wave_kernel<HD, 4>), grid, dim3(256), 0, s, a, p.slots, qscale); break;
-    case 2: SR_LAUNCH((paged_wave_kernel<HD, 2>), grid, dim3(128), 0, s, a, p.slots, qscale); break;
-    default: SR_LAUNCH((paged_wave_kernel<HD, 1>), grid, dim3(64), 0, s, a, p.slots, qscale); break;
+  int32_t* common = nullptr;
+  if (p.pre) {
+    common = reinterpret_cast<int32_t*>(a.part + partial_floats(a, p));
+    SR_LAUNCH(paged_common_kernel, dim3((a.rows + 3) / 4), dim3(256), 0, s, a, common);
+    SR_CHECK_LAUNCH();
+    launch_tile<HD, true>(a, common, p.pre, p.slots(), s);
   }
+  const dim3 grid(p.splits, a.hkv, a.rows);
+#define SR_PAGED_WAVE(NW)                                                                                          \
+  SR_LAUNCH((paged_wave_kernel<HD, NW>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, p.pre, \
+            p.slots(), qscale)
+  switch (p.nw) {
+    case 8: SR_PAGED_WAVE(8); break;
+    case 4: SR_PAGED_WAVE(4); break;
+    case 2: SR_PAGED_WAVE(2); break;
+    default: SR_PAGED_WAVE(1); break;
+  }
+#undef SR_PAGED_WAVE
   SR_CHECK_LAUNCH();
-  if (p.slots > 1) launch_merge<bf16_t, HD>(a, p.slots, s);
+  if (p.slots() > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
+}
+
+template <int HD>
+static void matrix_cores(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
+  if (p.kind == PAGED_WAVE) {
+    launch_wave<HD>(a, p, s);
+    return;
+  }
+  launch_tile<HD, false>(a, nullptr, p.splits, p.slots(), s);
+  if (p.slots() > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
 }
 
 void paged_attn(const PagedAttnArgs& a, hipStream_t s) {
   if (a.rows <= 0 || a.lr <= 0) return;
   const PagedPlan p = paged_plan(a);
-  if (p.kind == PAGED_WAVE) {
-    if (a.hd == 128) launch_wave<128>(a, p, s);
-    else launch_wave<64>(a, p, s);
+  if (p.kind != PAGED_VECTOR) {
+    if (a.hd == 128) matrix_cores<128>(a, p, s);
+    else matrix_cores<64>(a, p, s);
     return;
   }
   if (a.dtype == SR_BF16) vector_by_hd<bf16_t>(a, p, s);
