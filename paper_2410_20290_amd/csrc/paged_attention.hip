@@ -490,6 +490,7 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // XOR-swizzled in the LDS rows.  Two work-groups a CU.  With several splits a
 // work-group takes an even share of the blocks.
 constexpr int kTileStages = 4;
+constexpr float kStale = 8.f;
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE>
@@ -731,18 +732,23 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     const uint32_t out = gone >> (2 * (tile % kTileStages)) & 3u;
     if (key + 32 > all_end || (key < all_lo && key + 32 > a.sinks) || out) {   // (uniform) an edge
       asm volatile("");                        // (a branch, not selects on every block)
-      const int e0 = end_c - key - 4 * fh, l0 = lo_c - key - 4 * fh, s0 = a.sinks - key - 4 * fh;
+      // bit j: this lane's key j of the block (of the 32 from 4 fh on) is seen
+      const int k4 = key + 4 * fh;
+      auto below = [](int n) { return n >= 32 ? ~0u : (1u << imax(n, 0)) - 1u; };
+      uint32_t seen = below(end_c - k4) & (~below(lo_c - k4) | below(a.sinks - k4));
+      if (out & 1) seen &= 0xFFFF0000u;
+      if (out & 2) seen &= 0x0000FFFFu;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = 8 * (e >> 2) + (e & 3);
-        if (!(j < e0 && (j >= l0 || j < s0)) || (out >> (e >> 3) & 1u)) sc[e] = -INFINITY;
-      }
+      for (int e = 0; e < 16; ++e) sc[e] = (int)(seen << (31 - 8 * (e >> 2) - (e & 3))) < 0 ? sc[e] : -INFINITY;
     }
     float mt = sc[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
     mt = fmaxf(mt, other_half(mt));
-    if (__any(mt > m)) {
+    // Probabilities are relative to a maximum up to 2^kStale out of date: a
+    // rescaling of the accumulators costs as much as half a block's
+    // exponentials, and a wave's 32 columns would need one in most blocks.
+    if (__any(mt > m + kStale)) {
       const float mn = fmaxf(m, mt);
       const float corr = __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
