@@ -620,9 +620,17 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   };
   // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
   // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
-  // stored there.  A key nobody sees is replaced by one of its half that
-  // somebody does, a half without any by zeros.
+  // stored there, from a buffer resource at its 16-key half (no vector
+  // arithmetic where every key is seen).  A key nobody sees is replaced by one
+  // of its half that somebody does, a half without any by zeros.
   auto vswz = [](int k) { return HD == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2; };
+  uint32_t kcopy[DPW], vcopy[DPW];   // byte offsets in the half
+#pragma unroll
+  for (int i = 0; i < DPW; ++i) {
+    const int r = RPI * (wave + NW * i) + lane / CPK, sl = lane % CPK;
+    kcopy[i] = (uint32_t)((r & 15) * HD + 8 * (sl ^ (r & (CPK - 1)))) * 2;
+    vcopy[i] = (uint32_t)((r & 15) * HD + 8 * (sl ^ vswz(r))) * 2;
+  }
   uint32_t gone = 0;   // two bits a stage: halves that no page holds
   auto issue = [&](int tile) {
     if ((tile & 63) == 0) look_up(tile);
@@ -635,15 +643,18 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     const bool whole = kb.all32(k0);
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      const int r0 = RPI * (wave + NW * i), u = r0 >> 4;
-      const int r = r0 + lane / CPK, sl = lane % CPK, page = u ? pg[1] : pg[0];
-      int j = r & 15;
-      if (!whole && page >= 0) j = kb.safe(k0 + 16 * u, k0 + r) - (k0 + 16 * u);
-      const int64_t at = page < 0 ? 0 : page_offset(page, a.hkv, h, a.shift, k0 + 16 * u, HD);
-      const bf16_t* ks = page < 0 ? zero_keys : (const bf16_t*)a.kpool + at;
-      const bf16_t* vs = page < 0 ? zero_keys : (const bf16_t*)a.vpool + at;
-      dma16(reinterpret_cast<const char*>(ks + (j * HD + 8 * (sl ^ (r & (CPK - 1))))), kd + r0 * HD);
-      dma16(reinterpret_cast<const char*>(vs + (j * HD + 8 * (sl ^ vswz(r)))), vd + r0 * HD);
+      const int r0 = RPI * (wave + NW * i), u = r0 >> 4, page = u ? pg[1] : pg[0];
+      const int64_t at = page_offset(page, a.hkv, h, a.shift, k0 + 16 * u, HD);
+      const BufRsrc rk = buf_rsrc(page < 0 ? zero_keys : (const bf16_t*)a.kpool + at);
+      const BufRsrc rv = buf_rsrc(page < 0 ? zero_keys : (const bf16_t*)a.vpool + at);
+      uint32_t ko = kcopy[i], vo = vcopy[i];
+      if (!whole && page >= 0) {
+        const int r = r0 + lane / CPK, d = kb.safe(k0 + 16 * u, k0 + r) - (k0 + r);
+        ko += (uint32_t)(d * HD * 2);
+        vo += (uint32_t)(d * HD * 2);
+      }
+      dma16(rk, ko, 0, kd + r0 * HD);
+      dma16(rv, vo, 0, vd + r0 * HD);
     }
   };
   auto wait_barrier = [](auto n) {
@@ -682,23 +693,33 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
   };
-  // The scores `sc` of block `tile` (keys from `key` on) are there; the scores
-  // of the next block (K rows at `kn`) are formed into `sn`.  Per 16-key chunk:
-  // the K fragments and V of the chunk are read under the O MFMAs of the chunk
-  // before, then every score MFMA runs beside a share of the chunk's
-  // probabilities.
-  constexpr int KC = KS / 2;     // score MFMAs of a chunk
-  auto step = [&](int tile, f32x16& sc, f32x16& sn) {
-    const int key = kb.key0(i0 + tile);
-    const bf16_t* kn = lds + ((tile + 1) % kTileStages) * 2 * TILE;
-    uint32_t va[DT];
+  // The greatest score of each column.
+  auto peak = [](const f32x16& sc) {
+    float mt = sc[0];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) va[dt] = vbase[dt] + (uint32_t)(tile % kTileStages) * (2 * TILE * 2);
+    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
+    return fmaxf(mt, other_half(mt));
+  };
+  // Block `tile` in stage ST: its scores `sc`, their maxima mt (before masking)
+  // and the V of its first 16 keys (lo, hi) are there; the scores of the next
+  // block are formed into `sn`.  Per 16-key chunk every score product runs beside
+  // a share of the chunk's probabilities; K and the second chunk's V are read
+  // under the products before their use, the next block's first V and its scores'
+  // maxima under the last ones.
+  constexpr int KC = KS / 2;     // score products of a chunk
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  i16x4 lo[DT], hi[DT];
+  float mt = -INFINITY;
+  auto step = [&](auto stage, int tile, f32x16& sc, f32x16& sn) {
+    constexpr int ST = decltype(stage)::value, NX = (ST + 1) % kTileStages;
+    constexpr int VB = ST * 2 * TILE * 2, VN = NX * 2 * TILE * 2;   // bytes from vbase
+    const int key = kb.key0(i0 + tile);
     bf16x8 kf[KC], pf;
-    i16x4 lo[DT], hi[DT];
     auto read_k = [&](int c) {
 #pragma unroll
-      for (int s = 0; s < KC; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kn + koff[c * KC + s]);
+      for (int s = 0; s < KC; ++s)
+        kf[s] = *reinterpret_cast<const bf16x8*>(lds + (koff[c * KC + s] + NX * 2 * TILE));
     };
     auto scores = [&](int c) {
       __builtin_amdgcn_sched_barrier(0);
@@ -706,18 +727,17 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       for (int s = 0; s < KC; ++s) {
         sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[c * KC + s], sn, 0, 0, 0);
 #pragma unroll
-        for (int e = s * 8 / KC; e < (s + 1) * 8 / KC; ++e) {
-          const float p = __builtin_amdgcn_exp2f(sc[8 * c + e] - m);
-          l += p;
-          pf[e] = (__bf16)p;
-        }
+        for (int e = s * 8 / KC; e < (s + 1) * 8 / KC; ++e) pf[e] = (__bf16)__builtin_amdgcn_exp2f(sc[8 * c + e] - m);
       }
+      // (of the rounded ones, as the product has them)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[e], pf[e + 1]}, ones, l, false);
 #pragma unroll
       for (int s = 0; s < KC; ++s) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, 8 / KC, 0);
         __builtin_amdgcn_sched_group_barrier(0x400, 8 / KC, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 12 / KC, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 8 / KC, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
@@ -725,11 +745,9 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf, o[dt], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
     };
     read_k(0);
-    lds_read_tr16_pairs<DT, 0, 8 * HD * 2>(va, lo, hi);
-    const uint32_t out = gone >> (2 * (tile % kTileStages)) & 3u;
+    const uint32_t out = gone >> (2 * ST) & 3u;
     if (key + 32 > all_end || (key < all_lo && key + 32 > a.sinks) || out) {   // (uniform) an edge
       asm volatile("");                        // (a branch, not selects on every block)
       // bit j: this lane's key j of the block (of the 32 from 4 fh on) is seen
@@ -740,11 +758,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       if (out & 2) seen &= 0x0000FFFFu;
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e] = (int)(seen << (31 - 8 * (e >> 2) - (e & 3))) < 0 ? sc[e] : -INFINITY;
+      mt = peak(sc);
     }
-    float mt = sc[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
-    mt = fmaxf(mt, other_half(mt));
     // Probabilities are relative to a maximum up to 2^kStale out of date: a
     // rescaling of the accumulators costs as much as half a block's
     // exponentials, and a wave's 32 columns would need one in most blocks.
@@ -760,9 +775,13 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     scores(0);
     read_k(1);
     output();
-    lds_read_tr16_pairs<DT, 16 * HD * 2, 24 * HD * 2>(va, lo, hi);
+    __builtin_amdgcn_sched_barrier(0);
+    lds_read_tr16_pairs<DT, VB + 16 * HD * 2, VB + 24 * HD * 2>(vbase, lo, hi);
     scores(1);
     output();
+    mt = peak(sn);
+    __builtin_amdgcn_sched_barrier(0);
+    lds_read_tr16_pairs<DT, VN, VN + 8 * HD * 2>(vbase, lo, hi);
   };
   // Before block i: block i + 1 landed too (its first scores are formed under
   // block i; only the copies of i + 2 may still fly), and every wave is done
@@ -799,15 +818,19 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds + koff[s]);
       sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sa, 0, 0, 0);
     }
-    // two blocks a round; the scores formed past the last block are those of a
-    // stale buffer and never used
-    for (int tile = 0; tile < ntile; tile += 2) {
+    mt = peak(sa);
+    lds_read_tr16_pairs<DT, 0, 8 * HD * 2>(vbase, lo, hi);
+    // four blocks a round, a stage each; the scores formed past the last block
+    // are those of a stale buffer and never used
+    auto one = [&](auto stage, int tile, f32x16& sc, f32x16& sn) {
       if (tile > 0) sync(tile);
-      if (kb.key0(i0 + tile) < wend) step(tile, sa, sb);   // else past this wave's last query
-      if (tile + 1 < ntile) {
-        sync(tile + 1);
-        if (kb.key0(i0 + tile + 1) < wend) step(tile + 1, sb, sa);
-      }
+      if (kb.key0(i0 + tile) < wend) step(stage, tile, sc, sn);   // else past this wave's last query
+    };
+    for (int tile = 0; tile < ntile; tile += 4) {
+      one(std::integral_constant<int, 0>{}, tile, sa, sb);
+      if (tile + 1 < ntile) one(std::integral_constant<int, 1>{}, tile + 1, sb, sa);
+      if (tile + 2 < ntile) one(std::integral_constant<int, 2>{}, tile + 2, sa, sb);
+      if (tile + 3 < ntile) one(std::integral_constant<int, 3>{}, tile + 3, sb, sa);
     }
   }
   l += other_half(l);
