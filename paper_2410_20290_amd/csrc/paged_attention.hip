@@ -604,20 +604,28 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
         a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
   }
 
-  // The pages of blocks [64 c, 64 c + 64) of this split: lane i holds block
-  // 64 c + i's two, -1 for none.
+  // Where blocks [64 c, 64 c + 64) of this split lie: lane i holds, for block 64
+  // c + i, the address of its halves' keys (of zeros where no page holds one),
+  // and its flags, so that issuing a block's copies costs a few lane reads.
+  enum { GONE0 = 1, GONE1 = 2, PARTLY = 4 };   // no page; not every key is seen
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
-  int d0 = -1, d1 = -1;
+  uint32_t flags = 0, alo[2] = {0, 0}, ahi[2] = {0, 0};
   auto look_up = [&](int first) {
-    d0 = d1 = -1;
-    if (first + lane < ntile) {
-      const int k0 = kb.key0(i0 + first + lane);
-      const int p0 = kb.any16(k0) ? tab[k0 >> a.shift] : -1;
-      const int p1 = kb.any16(k0 + 16) ? tab[(k0 + 16) >> a.shift] : -1;
-      d0 = (uint32_t)p0 < (uint32_t)a.n_pages ? p0 : -1;
-      d1 = (uint32_t)p1 < (uint32_t)a.n_pages ? p1 : -1;
+    const int k0 = kb.key0(i0 + first + lane);
+    flags = kb.all32(k0) ? 0 : PARTLY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int k = k0 + 16 * u;
+      int page = first + lane < ntile && kb.any16(k) ? tab[k >> a.shift] : -1;
+      if ((uint32_t)page >= (uint32_t)a.n_pages) page = -1;
+      const bf16_t* at = page < 0 ? zero_keys
+                                  : (const bf16_t*)a.kpool + page_offset(page, a.hkv, h, a.shift, k, HD);
+      alo[u] = (uint32_t)reinterpret_cast<uintptr_t>(at);
+      ahi[u] = (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 32);
+      if (page < 0) flags |= u ? GONE1 : GONE0;
     }
   };
+  const int64_t k_to_v = reinterpret_cast<const char*>(a.vpool) - reinterpret_cast<const char*>(a.kpool);
   // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
   // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
   // stored there, from a buffer resource at its 16-key half (no vector
@@ -634,27 +642,31 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   uint32_t gone = 0;   // two bits a stage: halves that no page holds
   auto issue = [&](int tile) {
     if ((tile & 63) == 0) look_up(tile);
-    const int buf = tile % kTileStages;
+    const int buf = tile % kTileStages, at = tile & 63;
     bf16_t* kd = lds + buf * 2 * TILE;
     bf16_t* vd = kd + TILE;
-    const int pg[2] = {__builtin_amdgcn_readlane(d0, tile & 63), __builtin_amdgcn_readlane(d1, tile & 63)};
-    gone = (gone & ~(3u << (2 * buf))) | ((pg[0] < 0 ? 1u : 0u) | (pg[1] < 0 ? 2u : 0u)) << (2 * buf);
-    const int k0 = kb.key0(i0 + tile);
-    const bool whole = kb.all32(k0);
+    const uint32_t f = __builtin_amdgcn_readlane(flags, at);
+    gone = (gone & ~(3u << (2 * buf))) | (f & 3u) << (2 * buf);
+    const char* ks[2];
+    int64_t dv[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t lo = __builtin_amdgcn_readlane(alo[u], at), hi = __builtin_amdgcn_readlane(ahi[u], at);
+      ks[u] = reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+      dv[u] = f & (u ? GONE1 : GONE0) ? 0 : k_to_v;
+    }
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      const int r0 = RPI * (wave + NW * i), u = r0 >> 4, page = u ? pg[1] : pg[0];
-      const int64_t at = page_offset(page, a.hkv, h, a.shift, k0 + 16 * u, HD);
-      const BufRsrc rk = buf_rsrc(page < 0 ? zero_keys : (const bf16_t*)a.kpool + at);
-      const BufRsrc rv = buf_rsrc(page < 0 ? zero_keys : (const bf16_t*)a.vpool + at);
+      const int r0 = RPI * (wave + NW * i), u = r0 >> 4;
+      const char* src = u ? ks[1] : ks[0];
       uint32_t ko = kcopy[i], vo = vcopy[i];
-      if (!whole && page >= 0) {
-        const int r = r0 + lane / CPK, d = kb.safe(k0 + 16 * u, k0 + r) - (k0 + r);
+      if (f & PARTLY && !(f & (u ? GONE1 : GONE0))) {
+        const int k = kb.key0(i0 + tile) + r0 + lane / CPK, d = kb.safe(k & ~15, k) - k;
         ko += (uint32_t)(d * HD * 2);
         vo += (uint32_t)(d * HD * 2);
       }
-      dma16(rk, ko, 0, kd + r0 * HD);
-      dma16(rv, vo, 0, vd + r0 * HD);
+      dma16(buf_rsrc(src), ko, 0, kd + r0 * HD);
+      dma16(buf_rsrc(src + (u ? dv[1] : dv[0])), vo, 0, vd + r0 * HD);
     }
   };
   auto wait_barrier = [](auto n) {
