@@ -605,27 +605,38 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   }
 
   // Where blocks [64 c, 64 c + 64) of this split lie: lane i holds, for block 64
-  // c + i, the address of its halves' keys (of zeros where no page holds one),
-  // and its flags, so that issuing a block's copies costs a few lane reads.
-  enum { GONE0 = 1, GONE1 = 2, PARTLY = 4 };   // no page; not every key is seen
+  // c + i, the addresses of its halves' keys and values (of zeros where no page
+  // holds them) and its flags, so that issuing a block's copies costs a few lane
+  // reads: scalar instructions in a row cost a wave 5-8 cycles each.
+  enum {
+    GONE0 = 1, GONE1 = 2,   // no page holds the half
+    EDGE = 4,               // some column of the wave does not see every key
+    PAST = 8,               // no column of the wave sees a key
+    PARTLY = 16             // no column of the work-group sees some key
+  };
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
-  uint32_t flags = 0, alo[2] = {0, 0}, ahi[2] = {0, 0};
+  uint32_t flags = 0;
+  uint2 at[2][2];           // [keys, values][half]
   auto look_up = [&](int first) {
     const int k0 = kb.key0(i0 + first + lane);
     flags = kb.all32(k0) ? 0 : PARTLY;
+    if (k0 + 32 > all_end || (k0 < all_lo && k0 + 32 > a.sinks)) flags |= EDGE;
+    if (k0 >= wend) flags |= PAST;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int k = k0 + 16 * u;
       int page = first + lane < ntile && kb.any16(k) ? tab[k >> a.shift] : -1;
       if ((uint32_t)page >= (uint32_t)a.n_pages) page = -1;
-      const bf16_t* at = page < 0 ? zero_keys
-                                  : (const bf16_t*)a.kpool + page_offset(page, a.hkv, h, a.shift, k, HD);
-      alo[u] = (uint32_t)reinterpret_cast<uintptr_t>(at);
-      ahi[u] = (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 32);
-      if (page < 0) flags |= u ? GONE1 : GONE0;
+      const int64_t off = page < 0 ? 0 : page_offset(page, a.hkv, h, a.shift, k, HD);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const bf16_t* pool = page < 0 ? zero_keys : (const bf16_t*)(v ? a.vpool : a.kpool);
+        const uint64_t addr = reinterpret_cast<uintptr_t>(pool + off);
+        at[v][u] = make_uint2((uint32_t)addr, (uint32_t)(addr >> 32));
+      }
+      if (page < 0) flags |= EDGE | (u ? GONE1 : GONE0);
     }
   };
-  const int64_t k_to_v = reinterpret_cast<const char*>(a.vpool) - reinterpret_cast<const char*>(a.kpool);
   // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
   // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
   // stored there, from a buffer resource at its 16-key half (no vector
@@ -639,34 +650,41 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     kcopy[i] = (uint32_t)((r & 15) * HD + 8 * (sl ^ (r & (CPK - 1)))) * 2;
     vcopy[i] = (uint32_t)((r & 15) * HD + 8 * (sl ^ vswz(r))) * 2;
   }
-  uint32_t gone = 0;   // two bits a stage: halves that no page holds
-  auto issue = [&](int tile) {
+  uint32_t ring = 0;   // four flags for each stage
+  auto issue = [&](int tile, int buf) {
     if ((tile & 63) == 0) look_up(tile);
-    const int buf = tile % kTileStages, at = tile & 63;
+    const int from = tile & 63;
     bf16_t* kd = lds + buf * 2 * TILE;
-    bf16_t* vd = kd + TILE;
-    const uint32_t f = __builtin_amdgcn_readlane(flags, at);
-    gone = (gone & ~(3u << (2 * buf))) | (f & 3u) << (2 * buf);
-    const char* ks[2];
-    int64_t dv[2];
+    const uint32_t f = __builtin_amdgcn_readlane(flags, from);
+    ring = (ring & ~(15u << (4 * buf))) | (f & 15u) << (4 * buf);
+    auto source = [&](const uint2& v) {
+      const uint32_t lo = __builtin_amdgcn_readlane(v.x, from), hi = __builtin_amdgcn_readlane(v.y, from);
+      return buf_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo));
+    };
+    uint32_t ko[DPW], vo[DPW];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint32_t lo = __builtin_amdgcn_readlane(alo[u], at), hi = __builtin_amdgcn_readlane(ahi[u], at);
-      ks[u] = reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
-      dv[u] = f & (u ? GONE1 : GONE0) ? 0 : k_to_v;
+    for (int i = 0; i < DPW; ++i) {
+      ko[i] = kcopy[i];
+      vo[i] = vcopy[i];
+    }
+    if (f & PARTLY) {
+#pragma unroll
+      for (int i = 0; i < DPW; ++i) {
+        const int r0 = RPI * (wave + NW * i);
+        if (f & (r0 >> 4 ? GONE1 : GONE0)) continue;
+        const int k = kb.key0(i0 + tile) + r0 + lane / CPK, d = kb.safe(k & ~15, k) - k;
+        ko[i] += (uint32_t)(d * HD * 2);
+        vo[i] += (uint32_t)(d * HD * 2);
+      }
     }
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      const int r0 = RPI * (wave + NW * i), u = r0 >> 4;
-      const char* src = u ? ks[1] : ks[0];
-      uint32_t ko = kcopy[i], vo = vcopy[i];
-      if (f & PARTLY && !(f & (u ? GONE1 : GONE0))) {
-        const int k = kb.key0(i0 + tile) + r0 + lane / CPK, d = kb.safe(k & ~15, k) - k;
-        ko += (uint32_t)(d * HD * 2);
-        vo += (uint32_t)(d * HD * 2);
-      }
-      dma16(buf_rsrc(src), ko, 0, kd + r0 * HD);
-      dma16(buf_rsrc(src + (u ? dv[1] : dv[0])), vo, 0, vd + r0 * HD);
+      const int r0 = RPI * (wave + NW * i);
+      // (128 dims: the waves' copies i lie in half i; 64: a wave has one copy)
+      const int u = DPW == 2 ? i : r0 >> 4;
+      const uint2 ks = DPW == 2 ? at[0][i] : u ? at[0][1] : at[0][0], vs = DPW == 2 ? at[1][i] : u ? at[1][1] : at[1][0];
+      dma16(source(ks), ko[i], 0, kd + r0 * HD);
+      dma16(source(vs), vo[i], 0, kd + TILE + r0 * HD);
     }
   };
   auto wait_barrier = [](auto n) {
@@ -723,10 +741,9 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
   i16x4 lo[DT], hi[DT];
   float mt = -INFINITY;
-  auto step = [&](auto stage, int tile, f32x16& sc, f32x16& sn) {
+  auto step = [&](auto stage, int tile, uint32_t f, f32x16& sc, f32x16& sn) {
     constexpr int ST = decltype(stage)::value, NX = (ST + 1) % kTileStages;
     constexpr int VB = ST * 2 * TILE * 2, VN = NX * 2 * TILE * 2;   // bytes from vbase
-    const int key = kb.key0(i0 + tile);
     bf16x8 kf[KC], pf;
     auto read_k = [&](int c) {
 #pragma unroll
@@ -759,15 +776,14 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf, o[dt], 0, 0, 0);
     };
     read_k(0);
-    const uint32_t out = gone >> (2 * ST) & 3u;
-    if (key + 32 > all_end || (key < all_lo && key + 32 > a.sinks) || out) {   // (uniform) an edge
+    if (f & EDGE) {                            // (uniform)
       asm volatile("");                        // (a branch, not selects on every block)
       // bit j: this lane's key j of the block (of the 32 from 4 fh on) is seen
-      const int k4 = key + 4 * fh;
+      const int k4 = kb.key0(i0 + tile) + 4 * fh;
       auto below = [](int n) { return n >= 32 ? ~0u : (1u << imax(n, 0)) - 1u; };
       uint32_t seen = below(end_c - k4) & (~below(lo_c - k4) | below(a.sinks - k4));
-      if (out & 1) seen &= 0xFFFF0000u;
-      if (out & 2) seen &= 0x0000FFFFu;
+      if (f & GONE0) seen &= 0xFFFF0000u;
+      if (f & GONE1) seen &= 0x0000FFFFu;
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e] = (int)(seen << (31 - 8 * (e >> 2) - (e & 3))) < 0 ? sc[e] : -INFINITY;
       mt = peak(sc);
@@ -798,18 +814,18 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   // Before block i: block i + 1 landed too (its first scores are formed under
   // block i; only the copies of i + 2 may still fly), and every wave is done
   // with block i - 1, whose buffer takes block i + 3.
-  auto sync = [&](int tile) {
+  auto sync = [&](int tile, int next) {
     if (tile + 2 < ntile) wait_barrier(std::integral_constant<int, CPW>{});
     else wait_barrier(std::integral_constant<int, 0>{});
-    if (tile + kTileStages - 1 < ntile) issue(tile + kTileStages - 1);
+    if (tile + kTileStages - 1 < ntile) issue(tile + kTileStages - 1, next);
   };
   bf16_t* const slice = lds + wave * 32 * HD;
   if (ntile > 0) {
     // Blocks 0 and 1 go out first; the scaled bf16 queries pass through the
     // buffers of blocks 2 and 3 (a 32-row slice per wave, chunks placed like
     // K's) into fragments: lane holds Q[column fr][16 s + 8 fh .. + 8].
-    issue(0);
-    if (ntile > 1) issue(1);
+    issue(0, 0);
+    if (ntile > 1) issue(1, 1);
     bf16_t* qs = slice + 2 * 2 * TILE;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -823,8 +839,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     f32x16 sa, sb;
     zero(sa);
     wait_barrier(std::integral_constant<int, 0>{});   // blocks 0 and 1, and every wave's queries read
-    if (ntile > 2) issue(2);
-    if (ntile > 3) issue(3);
+    if (ntile > 2) issue(2, 2);
+    if (ntile > 3) issue(3, 3);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds + koff[s]);
@@ -835,8 +851,10 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     // four blocks a round, a stage each; the scores formed past the last block
     // are those of a stale buffer and never used
     auto one = [&](auto stage, int tile, f32x16& sc, f32x16& sn) {
-      if (tile > 0) sync(tile);
-      if (kb.key0(i0 + tile) < wend) step(stage, tile, sc, sn);   // else past this wave's last query
+      constexpr int ST = decltype(stage)::value;
+      if (tile > 0) sync(tile, (ST + kTileStages - 1) % kTileStages);
+      const uint32_t f = ring >> (4 * ST);
+      if (!(f & PAST)) step(stage, tile, f, sc, sn);
     };
     for (int tile = 0; tile < ntile; tile += 4) {
       one(std::integral_constant<int, 0>{}, tile, sa, sb);
