@@ -418,39 +418,49 @@ def reward_scores(gen: DeviceModel, rm: DeviceModel, prompt, p: sr_params, token
 SR_ROPE_PLAIN, SR_ROPE_LINEAR, SR_ROPE_BANDS = 0, 1, 2
 
 
-def _expect(t, name: str, dtypes, shape=None):
-    """t's checks: type, layout and (None: any size) shape."""
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} has type {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
-    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+def _expect(t, name: str, dtype, shape):
+    """t's checks (a call is a few microseconds: one comparison each)."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, contiguous; got {t.dtype}, "
+                         f"{tuple(t.shape)}, strides {t.stride()}")
 
 
-def _call(tensors, stream, call, need=0, scratch_type=None):
-    """call(stream, scratch) on the tensors' device; scratch: `need` elements
-    of scratch_type, allocated on that stream (None when need is 0)."""
+def _sizes(t, name: str, dtypes, dims: int):
+    """The shape of a contiguous tensor of any size."""
+    if t.dtype not in dtypes or t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {dims} dimensions of {' or '.join(map(str, dtypes))}, contiguous; got "
+                         f"{t.dtype}, {tuple(t.shape)}, strides {t.stride()}")
+    return t.shape
+
+
+def _run(tensors, stream, call, args, need=0, scratch_type=None, at=None):
+    """call(*args, stream) on the tensors' device; with `need` elements of
+    scratch, allocated on that stream, their address and number go in at
+    args[at:at]."""
     import torch
-    dev = tensors[0].device
-    if dev.type != "cuda":
+    first = tensors[0]
+    index = first.get_device()
+    if index < 0:
         raise ValueError("tensors must be on a GPU")
     for t in tensors:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != index:
             raise ValueError("tensors are on different devices")
-    if stream is not None and stream.device != dev:
+    if stream is not None and stream.device != first.device:
         raise ValueError("the stream is another device's")
-    if dev.index != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            return _call(tensors, stream, call, need, scratch_type)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _run(tensors, stream, call, args, need, scratch_type, at)
     scratch = None
     if need:
         if stream is None:
-            scratch = torch.empty(need, dtype=scratch_type, device=dev)
+            scratch = torch.empty(need, dtype=scratch_type, device=first.device)
         else:
             with torch.cuda.stream(stream):
-                scratch = torch.empty(need, dtype=scratch_type, device=dev)
-    _check(call(_stream(stream), _ptr(scratch)))
+                scratch = torch.empty(need, dtype=scratch_type, device=first.device)
+    if at is not None:
+        args = (*args[:at], _ptr(scratch), need, *args[at:])
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    _check(call(*args, raw))
 
 
 def _cache_types():
@@ -460,9 +470,10 @@ def _cache_types():
 
 def _pool_args(pool):
     """(ctypes arguments, n_pages) of a pool [layers][2][n_pages][hkv][page_tokens][hd]."""
-    _expect(pool, "pool", _cache_types(), (None, 2, None, None, None, None))
-    nl, _, n_pages, hkv, pt, hd = pool.shape
-    return (_ptr(pool), n_pages * hkv * pt * hd, nl, hkv, hd, pool.element_size(), pt, n_pages), n_pages
+    nl, two, n_pages, hkv, pt, hd = _sizes(pool, "pool", _cache_types(), 6)
+    if two != 2:
+        raise ValueError(f"pool has shape {tuple(pool.shape)}, expected [layers][2][n_pages][hkv][page_tokens][hd]")
+    return (pool.data_ptr(), n_pages * hkv * pt * hd, nl, hkv, hd, pool.element_size(), pt, n_pages), n_pages
 
 
 def page_fork(table, lens, parent, page_tokens: int, table_out, lens_out, refs_out, window: int = 0, sinks: int = 0,
@@ -470,28 +481,25 @@ def page_fork(table, lens, parent, page_tokens: int, table_out, lens_out, refs_o
     """sr_page_fork: table int32 [rows][max_pages], lens [rows], parent [new
     rows] -> table_out [new rows][max_pages], lens_out, refs_out [n_pages]."""
     import torch
-    i32 = (torch.int32,)
-    _expect(table, "table", i32, (None, None))
-    rows, mp = table.shape
+    i32 = torch.int32
+    rows, mp = _sizes(table, "table", (i32,), 2)
+    n, = _sizes(parent, "parent", (i32,), 1)
+    n_pages, = _sizes(refs_out, "refs_out", (i32,), 1)
     _expect(lens, "lens", i32, (rows,))
-    _expect(parent, "parent", i32, (None,))
-    n = parent.shape[0]
     _expect(table_out, "table_out", i32, (n, mp))
     _expect(lens_out, "lens_out", i32, (n,))
-    _expect(refs_out, "refs_out", i32, (None,))
-    _call((refs_out, table, lens, parent, table_out, lens_out), stream, lambda s, _: lib().sr_page_fork(
-        _ptr(table), _ptr(lens), rows, mp, _ptr(parent), n, page_tokens, refs_out.shape[0], window, sinks,
-        _ptr(table_out), _ptr(lens_out), _ptr(refs_out), s))
+    _run((refs_out, table, lens, parent, table_out, lens_out), stream, lib().sr_page_fork,
+         (table.data_ptr(), lens.data_ptr(), rows, mp, parent.data_ptr(), n, page_tokens, n_pages, window, sinks,
+          table_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr()))
 
 
 def page_reserve(pool, table, lens, refs, n_add, table_out, lens_out, refs_out, granted, info, stream=None):
     """sr_page_reserve: room for n_add tokens (int32 [rows], or one number for
     every row).  table_out, lens_out and refs_out may be the inputs."""
     import torch
-    i32 = (torch.int32,)
+    i32 = torch.int32
     pa, n_pages = _pool_args(pool)
-    _expect(table, "table", i32, (None, None))
-    rows, mp = table.shape
+    rows, mp = _sizes(table, "table", (i32,), 2)
     for t, name, shape in ((lens, "lens", (rows,)), (refs, "refs", (n_pages,)), (table_out, "table_out", (rows, mp)),
                            (lens_out, "lens_out", (rows,)), (refs_out, "refs_out", (n_pages,)),
                            (granted, "granted", (rows,)), (info, "info", (4,))):
@@ -499,28 +507,27 @@ def page_reserve(pool, table, lens, refs, n_add, table_out, lens_out, refs_out, 
     each = n_add if torch.is_tensor(n_add) else None
     if each is not None:
         _expect(each, "n_add", i32, (rows,))
-    need = int(lib().sr_page_reserve_scratch(rows, mp, n_pages))
-    _call((pool, table, lens, refs, each, table_out, lens_out, refs_out, granted, info), stream,
-          lambda s, w: lib().sr_page_reserve(*pa, _ptr(table), _ptr(lens), _ptr(refs), rows, mp, _ptr(each),
-                                             0 if each is not None else int(n_add), _ptr(table_out), _ptr(lens_out),
-                                             _ptr(refs_out), _ptr(granted), _ptr(info), w, need, s), need, torch.int32)
+    L = lib()
+    _run((pool, table, lens, refs, each, table_out, lens_out, refs_out, granted, info), stream, L.sr_page_reserve,
+         (*pa, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), rows, mp, _ptr(each), 0 if each is not None else int(n_add),
+          table_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(), granted.data_ptr(), info.data_ptr()),
+         L.sr_page_reserve_scratch(rows, mp, n_pages), i32, 20)
 
 
 def page_compact(pool, table, lens, refs, table_out, refs_out, info, stream=None):
     """sr_page_compact: live pages to the front of the pool, in place.
     table_out and refs_out may be the inputs."""
     import torch
-    i32 = (torch.int32,)
+    i32 = torch.int32
     pa, n_pages = _pool_args(pool)
-    _expect(table, "table", i32, (None, None))
-    rows, mp = table.shape
+    rows, mp = _sizes(table, "table", (i32,), 2)
     for t, name, shape in ((lens, "lens", (rows,)), (refs, "refs", (n_pages,)), (table_out, "table_out", (rows, mp)),
                            (refs_out, "refs_out", (n_pages,)), (info, "info", (4,))):
         _expect(t, name, i32, shape)
-    need = int(lib().sr_page_compact_scratch(n_pages))
-    _call((pool, table, lens, refs, table_out, refs_out, info), stream,
-          lambda s, w: lib().sr_page_compact(*pa, _ptr(table), _ptr(lens), _ptr(refs), rows, mp, _ptr(table_out),
-                                             _ptr(refs_out), _ptr(info), w, need, s), need, torch.int32)
+    L = lib()
+    _run((pool, table, lens, refs, table_out, refs_out, info), stream, L.sr_page_compact,
+         (*pa, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), rows, mp, table_out.data_ptr(), refs_out.data_ptr(),
+          info.data_ptr()), L.sr_page_compact_scratch(n_pages), i32, 16)
 
 
 def rope_frequencies(rot_dim: int, theta: float, scaling: int = SR_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
@@ -535,16 +542,14 @@ def _layer_args(kpool, vpool, table, lens, n_new):
     """(dtype, rows, max_pages, hkv, page_tokens, hd, n_pages) of one layer's
     blocks [n_pages][hkv][page_tokens][hd] and the rows' table."""
     import torch
-    i32 = (torch.int32,)
-    _expect(kpool, "kpool", _cache_types(), (None, None, None, None))
-    _expect(vpool, "vpool", (kpool.dtype,), tuple(kpool.shape))
-    _expect(table, "table", i32, (None, None))
-    rows, mp = table.shape
+    i32 = torch.int32
+    n_pages, hkv, pt, hd = _sizes(kpool, "kpool", _cache_types(), 4)
+    _expect(vpool, "vpool", kpool.dtype, kpool.shape)
+    rows, mp = _sizes(table, "table", (i32,), 2)
     _expect(lens, "lens", i32, (rows,))
     if n_new is not None:
         _expect(n_new, "n_new", i32, (rows,))
-    n_pages, hkv, pt, hd = kpool.shape
-    return SR_F32 if kpool.dtype == torch.float32 else SR_BF16, rows, mp, hkv, pt, hd, n_pages
+    return SR_F32 if kpool.dtype is torch.float32 else SR_BF16, rows, mp, hkv, pt, hd, n_pages
 
 
 def page_append(qkv, freqs, table, lens, kpool, vpool, q, n_new=None, interleaved: bool = False, stream=None):
@@ -553,17 +558,13 @@ def page_append(qkv, freqs, table, lens, kpool, vpool, q, n_new=None, interleave
     rows' pages of one layer's kpool, vpool [n_pages][hkv][page_tokens][hd]."""
     import torch
     dtype, rows, mp, hkv, pt, hd, n_pages = _layer_args(kpool, vpool, table, lens, n_new)
-    _expect(q, "q", (torch.float32,), (rows, None, None, hd))
-    lr, hq = q.shape[1:3]
-    _expect(qkv, "qkv", (torch.float32,), (rows, lr, (hq + 2 * hkv) * hd))
-    rot = 0
-    if freqs is not None:
-        _expect(freqs, "freqs", (torch.float64,), (None,))
-        rot = 2 * freqs.shape[0]
-    _call((qkv, freqs, table, lens, kpool, vpool, q, n_new), stream,
-          lambda s, _: lib().sr_page_append(dtype, hd, hq, hkv, rows, lr, _ptr(qkv), _ptr(freqs), rot, int(interleaved),
-                                            _ptr(kpool), _ptr(vpool), pt, n_pages, _ptr(table), mp, _ptr(lens),
-                                            _ptr(n_new), _ptr(q), s))
+    _, lr, hq, _ = _sizes(q, "q", (torch.float32,), 4)
+    _expect(q, "q", torch.float32, (rows, lr, hq, hd))
+    _expect(qkv, "qkv", torch.float32, (rows, lr, (hq + 2 * hkv) * hd))
+    rot = 0 if freqs is None else 2 * _sizes(freqs, "freqs", (torch.float64,), 1)[0]
+    _run((qkv, freqs, table, lens, kpool, vpool, q, n_new), stream, lib().sr_page_append,
+         (dtype, hd, hq, hkv, rows, lr, qkv.data_ptr(), _ptr(freqs), rot, 1 if interleaved else 0, kpool.data_ptr(),
+          vpool.data_ptr(), pt, n_pages, table.data_ptr(), mp, lens.data_ptr(), _ptr(n_new), q.data_ptr()))
 
 
 def paged_attention(q, kpool, vpool, table, lens, out, n_new=None, window: int = 0, sinks: int = 0, shared: int = 0,
@@ -573,16 +574,19 @@ def paged_attention(q, kpool, vpool, table, lens, out, n_new=None, window: int =
     type (bf16 may travel as int16).  max_len None: the table's capacity."""
     import torch
     dtype, rows, mp, hkv, pt, hd, n_pages = _layer_args(kpool, vpool, table, lens, n_new)
-    _expect(q, "q", (torch.float32,), (rows, None, None, hd))
-    lr, hq = q.shape[1:3]
-    _expect(out, "out", (torch.float32,) if dtype == SR_F32 else (torch.bfloat16, torch.int16), (rows, lr, hq * hd))
+    _, lr, hq, _ = _sizes(q, "q", (torch.float32,), 4)
+    _expect(q, "q", torch.float32, (rows, lr, hq, hd))
+    if out.dtype is not kpool.dtype and (dtype == SR_F32 or out.dtype not in (torch.bfloat16, torch.int16)):
+        raise ValueError(f"out has type {out.dtype}, the cache {kpool.dtype}")
+    _expect(out, "out", out.dtype, (rows, lr, hq * hd))
     if max_len is None:
-        max_len = mp * pt
-    need = int(lib().sr_paged_attention_scratch(dtype, hd, hq, hkv, rows, lr, pt, mp, window, sinks, shared, max_len))
-    _call((q, kpool, vpool, table, lens, out, n_new), stream,
-          lambda s, w: lib().sr_paged_attention(dtype, hd, hq, hkv, rows, lr, _ptr(q), _ptr(kpool), _ptr(vpool), pt,
-                                                n_pages, _ptr(table), mp, _ptr(lens), _ptr(n_new), window, sinks,
-                                                shared, max_len, _ptr(out), w, need, s), need, torch.float32)
+        max_len = max(1, mp * pt)
+    L = lib()
+    _run((q, kpool, vpool, table, lens, out, n_new), stream, L.sr_paged_attention,
+         (dtype, hd, hq, hkv, rows, lr, q.data_ptr(), kpool.data_ptr(), vpool.data_ptr(), pt, n_pages, table.data_ptr(), mp,
+          lens.data_ptr(), _ptr(n_new), window, sinks, shared, max_len, out.data_ptr()),
+         L.sr_paged_attention_scratch(dtype, hd, hq, hkv, rows, lr, pt, mp, window, sinks, shared, max_len),
+         torch.float32, 20)
 
 
 def token_logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=None, temperature: float = 1.0,
@@ -602,10 +606,9 @@ def token_logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logp
                                 (top_ids, "top_ids", torch.int32, (rows, top)),
                                 (top_logprobs, "top_logprobs", torch.float32, (rows, top))):
         if t is not None:
-            _expect(t, name, (typ,), shape)
-    need = int(lib().sr_token_logprobs_scratch(rows, vocab, top))
-    _call((logits, tokens, logprob, entropy, top_ids, top_logprobs), stream,
-          lambda s, w: lib().sr_token_logprobs(SR_F32 if logits.dtype == torch.float32 else SR_BF16, _ptr(logits),
-                                               stride, rows, vocab, temperature, _ptr(tokens), top, _ptr(logprob),
-                                               _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), w, need, s),
-          need, torch.float32)
+            _expect(t, name, typ, shape)
+    L = lib()
+    _run((logits, tokens, logprob, entropy, top_ids, top_logprobs), stream, L.sr_token_logprobs,
+         (SR_F32 if logits.dtype is torch.float32 else SR_BF16, logits.data_ptr(), stride, rows, vocab, temperature,
+          _ptr(tokens), top, _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs)),
+         L.sr_token_logprobs_scratch(rows, vocab, top), torch.float32, 12)
