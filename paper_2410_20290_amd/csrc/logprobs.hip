@@ -8,6 +8,7 @@
 // bits above its inverted index, so that "larger" is "more likely, then lower
 // index" and no order of merging can change a result.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -81,17 +82,24 @@ struct Tile {
   }
 };
 
-// The best `keep` of a wave's n <= 2 * 64 listed words, sorted, to the front of
+// The best `keep` of a wave's n <= kLpList listed words, sorted, to the front of
 // the list; returns their number.  Lane l ranks words l and l + 64 by counting
-// the larger ones (words are distinct).
+// the larger ones (words are distinct), eight at a time.  The list has room for
+// eight more.
 __device__ int list_sort(uint64_t* list, int n, int keep) {
   const int lane = threadIdx.x & 63;
+  if (lane < 8) list[n + lane] = 0;   // (larger than nothing)
   const uint64_t a = lane < n ? list[lane] : 0, b = lane + 64 < n ? list[lane + 64] : 0;
   int ra = 0, rb = 0;
-  for (int i = 0; i < n; ++i) {
-    const uint64_t w = list[i];
-    ra += w > a ? 1 : 0;
-    rb += w > b ? 1 : 0;
+  for (int i = 0; i < n; i += 8) {
+    uint64_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = list[i + j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      ra += w[j] > a ? 1 : 0;
+      rb += w[j] > b ? 1 : 0;
+    }
   }
   __builtin_amdgcn_wave_barrier();   // (every lane has read before one writes: a wave's LDS operations are in order)
   if (lane < n && ra < keep) list[ra] = a;
@@ -100,20 +108,47 @@ __device__ int list_sort(uint64_t* list, int n, int keep) {
   return min(n, keep);
 }
 
+// The largest of the wave's values, by DPP: within rows of 16 lanes, then from
+// row to row; lane 63 ends up with it.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  auto step = [&](auto ctrl) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  step(std::integral_constant<int, 0x111>{});   // row_shr 1, 2, 4, 8
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x118>{});
+  step(std::integral_constant<int, 0x142>{});   // row_bcast 15, 31
+  step(std::integral_constant<int, 0x143>{});
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 // Partial results of a chunk: max, S, t, and `top` sorted words.
 __host__ __device__ inline int64_t chunk_floats(int top) { return 4 + 2 * (int64_t)top; }
 
-// What a row's sums and best words give.
+// A row's given token and its logit, read ahead of the sums.
+struct Given {
+  int tok;
+  float x;
+};
 template <typename T>
-__device__ void write_row(const LogprobArgs& a, int r, Sums s, float inv_t) {
+__device__ __forceinline__ Given given(const LogprobArgs& a, int r) {
+  Given g{-1, 0.f};
+  if (a.logprob) {
+    g.tok = a.tokens[r];
+    if ((uint32_t)g.tok < (uint32_t)a.vocab)
+      g.x = seen_logit(to_f32<T>(((const T*)a.logits + r * a.row_stride)[g.tok]));
+  }
+  return g;
+}
+// What a row's sums and best words give.
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, Given g, Sums s, float inv_t) {
   const bool none = s.m == -INFINITY;
   const float ls = none ? 0.f : logf(s.s);
   if (a.logprob) {
-    const int tok = a.tokens[r];
     float lp = __uint_as_float(0x7FC00000u);
-    if (tok == -1) lp = 0.f;
-    else if ((uint32_t)tok < (uint32_t)a.vocab)
-      lp = none ? -INFINITY : scaled(seen_logit(to_f32<T>(((const T*)a.logits + r * a.row_stride)[tok])), s.m, inv_t) - ls;
+    if (g.tok == -1) lp = 0.f;
+    else if ((uint32_t)g.tok < (uint32_t)a.vocab) lp = none ? -INFINITY : scaled(g.x, s.m, inv_t) - ls;
     a.logprob[r] = lp;
   }
   if (a.entropy) a.entropy[r] = none ? 0.f : ls - 0.6931471805599453f * (s.t / s.s);
@@ -130,7 +165,7 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int i, ui
 template <typename T, bool VEC, bool TOP>
 __global__ void __launch_bounds__(64 * kLpWaves)
 logprob_kernel(LogprobArgs a, int chunks, int chunk_len, float k, float inv_t) {
-  __shared__ uint64_t lists[kLpWaves][kLpList];
+  __shared__ uint64_t lists[kLpWaves][kLpList + 8];
   __shared__ Sums wsums[kLpWaves];
   __shared__ int wcount[kLpWaves];
   const int r = blockIdx.x / chunks, chunk = blockIdx.x - r * chunks;
@@ -140,6 +175,13 @@ logprob_kernel(LogprobArgs a, int chunks, int chunk_len, float k, float inv_t) {
   uint64_t* list = lists[wave];
   int n = 0;                      // listed words (uniform in the wave)
   uint64_t floor_word = 0;        // words below it are not among the best
+  float floor_value = -INFINITY;  // nor are values below it
+  auto raise = [&](uint64_t w) {
+    if (w <= floor_word) return;
+    floor_word = w;
+    const float f = word_value(w);
+    floor_value = f == f ? f : -INFINITY;   // (bits below -inf's read as a NaN)
+  };
   bool first = true;
   Sums s{-INFINITY, 0.f, 0.f};
   float v[16], nx[16];
@@ -183,28 +225,32 @@ logprob_kernel(LogprobArgs a, int chunks, int chunk_len, float k, float inv_t) {
         // wherever there are that many; else the bound stays 0).
         first = false;
         const uint32_t key = (uint32_t)(entry_word(mt, 0) >> 32);
-        uint32_t t = 0;
+        uint32_t t = 0;   // (its upper 16 bits are enough)
 #pragma unroll
-        for (int b = 31; b >= 0; --b) {
+        for (int b = 31; b >= 16; --b) {
           const uint32_t c = t | (1u << b);
           if (__popcll(__ballot(key >= c)) >= a.top) t = c;
         }
-        floor_word = (uint64_t)t << 32;
+        raise((uint64_t)t << 32);
       }
-      if (__any(entry_word(mt, 0) >= floor_word)) {   // (index 0: the largest word of that value)
+      if (__any(mt >= floor_value)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
+          uint64_t in = __ballot(seen_logit(v[e]) >= floor_value);   // (as values: ties are decided below)
+          if (in == 0) continue;
           const int i = Tile<T, VEC>::index(base, e, lane);
           const uint64_t w = entry_word(seen_logit(v[e]), i);
-          uint64_t in = __ballot(i < c1 && w >= floor_word);
-          if (in == 0) continue;
           if (n + __popcll(in) > kLpList) {
             n = list_sort(list, n, a.top);
-            if (n == a.top) floor_word = max(floor_word, list[n - 1]);
-            in = __ballot(i < c1 && w >= floor_word);
+            if (n == a.top) raise(list[n - 1]);
           }
+          in = __ballot(i < c1 && w >= floor_word);
           if (i < c1 && w >= floor_word) list[n + __popcll(in & ((1ull << lane) - 1))] = w;
           n += __popcll(in);
+        }
+        if (n >= a.top + 16) {   // (a higher floor saves the next tiles' candidates)
+          n = list_sort(list, n, a.top);
+          raise(list[n - 1]);
         }
       }
     }
@@ -235,7 +281,7 @@ logprob_kernel(LogprobArgs a, int chunks, int chunk_len, float k, float inv_t) {
     n = list_sort(list, n, a.top);
   }
   if (chunks == 1) {
-    if (lane == 0) write_row<T>(a, r, s, inv_t);
+    if (lane == 0) write_row(a, r, given<T>(a, r), s, inv_t);
     if (TOP && lane < n) write_top(a, r, lane, list[lane], s, inv_t);
     return;
   }
@@ -260,6 +306,7 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a, int chu
   const int r = blockIdx.x, lane = threadIdx.x;
   const int64_t stride = chunk_floats(a.top);
   const float* row = a.scratch + (int64_t)r * chunks * stride;
+  const Given g = given<T>(a, r);
 #pragma unroll 8
   for (int i = lane; i < chunks * a.top; i += 64) {   // (those past a chunk's number are never taken)
     const int c = i / a.top;
@@ -276,18 +323,15 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a, int chu
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1)
     s = join(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.s, o, 64), __shfl_xor(s.t, o, 64)}, k);
-  if (lane == 0) write_row<T>(a, r, s, inv_t);
+  if (lane == 0) write_row(a, r, g, s, inv_t);
   if (a.top == 0) return;
   __syncthreads();
   int at = 0;
   uint64_t head = n > 0 ? words[lane * a.top] : 0, mine = 0;
   for (int i = 0; i < a.top; ++i) {
-    uint64_t best = head;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t u = ((uint64_t)__shfl_xor((uint32_t)(best >> 32), o, 64) << 32) | __shfl_xor((uint32_t)best, o, 64);
-      best = max(best, u);
-    }
+    const uint32_t hi = wave_max_u32((uint32_t)(head >> 32));
+    const uint32_t lo = wave_max_u32((uint32_t)(head >> 32) == hi ? (uint32_t)head : 0);
+    const uint64_t best = (uint64_t)hi << 32 | lo;
     if (lane == i) mine = best;
     if (head == best) {   // (one lane: words are distinct, and top <= vocab of them exist)
       ++at;
