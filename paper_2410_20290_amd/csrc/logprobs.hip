@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a, int chu
 
 // Chunks of a row: of whole rounds of the waves' tiles, enough for about
 // kLpTarget work-groups.
-constexpr int kLpTarget = 2048;
+constexpr int kLpTarget = 1024;
 static int logprob_chunk_len(int rows, int vocab) {
   const int round = kLpWaves * kLpTile;
   const int rounds = (vocab + round - 1) / round;
