@@ -13,7 +13,6 @@ namespace sr {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
-constexpr int kPlanRows = kPageMaxRows / kPlanThreads;   // rows of a thread of the plan kernel
 
 __device__ __forceinline__ bool is_page(int pg, int n_pages) { return (uint32_t)pg < (uint32_t)n_pages; }
 __device__ __forceinline__ int pages_of(int tokens, int shift) { return (tokens + (1 << shift) - 1) >> shift; }
@@ -39,27 +38,100 @@ __device__ int plan_scan(int v, int* wsum, int* total) {
   return off + inc - v;
 }
 
+// The same of two counts below 2^31 each, in one round: x in the low half.
+__device__ int2 plan_scan2(int2 v, uint64_t* wsum, int2* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t inc = (uint64_t)(uint32_t)v.y << 32 | (uint32_t)v.x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t lo = __shfl_up((uint32_t)inc, o, 64), hi = __shfl_up((uint32_t)(inc >> 32), o, 64);
+    if (lane >= o) inc += (uint64_t)hi << 32 | lo;
+  }
+  __syncthreads();
+  if (lane == 63) wsum[wave] = inc;
+  __syncthreads();
+  uint64_t off = 0, tot = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const uint64_t x = wsum[w];
+    if (w < wave) off += x;
+    tot += x;
+  }
+  *total = make_int2((int)(uint32_t)tot, (int)(tot >> 32));
+  off += inc;
+  return make_int2((int)(uint32_t)off - v.x, (int)(off >> 32) - v.y);
+}
+
 // -------------------------------------------------------------------- fork
+// Entries i, i + step, .. (U of them, those below n) of the new table, and their
+// rows' lengths; the parents, lengths and entries of all are loaded together.
+template <int U>
+__device__ __forceinline__ void forked_entries(const PageForkArgs& a, int64_t i, int64_t step, int64_t n, int (&pg)[U],
+                                               int (&len)[U]) {
+  int par[U], c[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t k = i + u * step < n ? i + u * step : n - 1;
+    const int j = (int)(k / a.max_pages);
+    c[u] = (int)(k - (int64_t)j * a.max_pages);
+    par[u] = a.parent[j];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) len[u] = (uint32_t)par[u] < (uint32_t)a.rows ? a.lens[par[u]] : 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    len[u] = clamp_len(len[u], a.max_pages, a.shift);
+    // out of every later token's sight: the next one sits at position len
+    const bool behind = ((c[u] + 1) << a.shift) <= window_start(len[u], a.window) && (c[u] << a.shift) >= a.sinks;
+    const bool there = c[u] < pages_of(len[u], a.shift) && !behind;
+    pg[u] = there ? a.table[(int64_t)par[u] * a.max_pages + c[u]] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (!is_page(pg[u], a.n_pages)) pg[u] = -1;
+}
+
+// Small tables and pools, which take no longer than a launch: one work-group,
+// the counts in LDS.
+constexpr int kForkSmallPages = 16384, kForkSmallEntries = 32768;
+__global__ void __launch_bounds__(kPlanThreads) fork_small_kernel(PageForkArgs a) {
+  __shared__ int refs[kForkSmallPages];
+  for (int p = threadIdx.x; p < a.n_pages; p += kPlanThreads) refs[p] = 0;
+  __syncthreads();
+  const int n = a.new_rows * a.max_pages;
+  constexpr int U = 8;
+  for (int i = threadIdx.x; i < n; i += U * kPlanThreads) {
+    int pg[U], len[U];
+    forked_entries<U>(a, i, kPlanThreads, n, pg, len);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = i + u * kPlanThreads;
+      if (k >= n) break;
+      if (pg[u] >= 0) atomicAdd(&refs[pg[u]], 1);
+      a.table_out[k] = pg[u];
+      if (k % a.max_pages == 0) a.lens_out[k / a.max_pages] = len[u];
+    }
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < a.n_pages; p += kPlanThreads) a.refs_out[p] = refs[p];
+}
+
 // One thread per entry of the new table; the counts start at 0.
 __global__ void __launch_bounds__(256) fork_table_kernel(PageForkArgs a) {
   const int64_t tid = (int64_t)blockIdx.x * 256 + threadIdx.x, nthr = (int64_t)gridDim.x * 256;
   for (int64_t p = tid; p < a.n_pages; p += nthr) a.refs_out[p] = 0;
   const int64_t n = (int64_t)a.new_rows * a.max_pages;
-  for (int64_t i = tid; i < n; i += nthr) {
-    const int j = (int)(i / a.max_pages), c = (int)(i - (int64_t)j * a.max_pages);
-    const int par = a.parent[j];
-    int pg = -1, len = 0;
-    if ((uint32_t)par < (uint32_t)a.rows) {
-      len = clamp_len(a.lens[par], a.max_pages, a.shift);
-      if (c < pages_of(len, a.shift)) {
-        pg = a.table[(int64_t)par * a.max_pages + c];
-        // out of every later token's sight: the next one sits at position len
-        const bool behind = ((c + 1) << a.shift) <= window_start(len, a.window) && (c << a.shift) >= a.sinks;
-        if (!is_page(pg, a.n_pages) || behind) pg = -1;
-      }
+  constexpr int U = 4;
+  for (int64_t i = tid; i < n; i += U * nthr) {
+    int pg[U], len[U];
+    forked_entries<U>(a, i, nthr, n, pg, len);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = i + u * nthr;
+      if (k >= n) break;
+      a.table_out[k] = pg[u];
+      if (k % a.max_pages == 0) a.lens_out[k / a.max_pages] = len[u];
     }
-    a.table_out[i] = pg;
-    if (c == 0) a.lens_out[j] = len;
   }
 }
 
@@ -90,6 +162,11 @@ __global__ void __launch_bounds__(256) fork_count_kernel(const int32_t* __restri
 }
 
 void page_fork(const PageForkArgs& a, hipStream_t s) {
+  if (a.n_pages <= kForkSmallPages && (int64_t)a.new_rows * a.max_pages <= kForkSmallEntries) {
+    SR_LAUNCH(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    SR_CHECK_LAUNCH();
+    return;
+  }
   const int64_t n = std::max<int64_t>((int64_t)a.new_rows * a.max_pages, a.n_pages);
   SR_LAUNCH(fork_table_kernel, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, s, a);
   SR_CHECK_LAUNCH();
@@ -102,30 +179,31 @@ void page_fork(const PageForkArgs& a, hipStream_t s) {
 
 // ----------------------------------------------------------------- reserve
 // What the plan leaves for the second launch, per row: the column of its first
-// new entry, their number, where they start in the list of free pages, and the
-// new length; and the pages to copy.
+// new entry, their number, where they start in the list of free pages, its length
+// and the tokens to add; and the pages to copy.  (info says whether it stands.)
 struct ReservePlan {
-  int32_t *start, *need, *first, *new_len;   // [rows]
-  int32_t *src, *at, *part;                  // [rows] pairs: page, index into free, filled slots
+  int32_t *start, *need, *first, *len, *add;   // [rows]
+  int32_t *src, *at, *part;                    // [rows] pairs: page, index into free, filled slots
   int32_t* free;                             // [n_pages]
 };
-constexpr int kReserveArrays = 7;
+constexpr int kReserveArrays = 8;
 __host__ __device__ inline ReservePlan reserve_plan(int32_t* scratch, int rows) {
   ReservePlan p;
   p.start = scratch;
   p.need = scratch + rows;
   p.first = scratch + 2 * rows;
-  p.new_len = scratch + 3 * rows;
-  p.src = scratch + 4 * rows;
-  p.at = scratch + 5 * rows;
-  p.part = scratch + 6 * rows;
+  p.len = scratch + 3 * rows;
+  p.add = scratch + 4 * rows;
+  p.src = scratch + 5 * rows;
+  p.at = scratch + 6 * rows;
+  p.part = scratch + 7 * rows;
   p.free = scratch + kReserveArrays * rows;
   return p;
 }
 
 // A hash table in LDS counts, for every part-filled last page that more than
 // one entry names, the rows that add tokens to it, and finds the lowest.
-constexpr int kHashBits = 13, kHashSize = 1 << kHashBits;   // twice the rows: probing ends
+constexpr int kHashSize = 2 * kPageMaxRows;   // twice the rows: probing ends
 
 // Work-group 0 plans; the others copy the table and the counts meanwhile (the
 // second launch writes what changes).
@@ -145,107 +223,123 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(PageReserveA
     }
     return;
   }
-  __shared__ int hkey[kHashSize], hcount[kHashSize], hlow[kHashSize];
-  __shared__ int wsum[kPlanWaves];
+  __shared__ int hkey[kHashSize], hcount[kHashSize], hlow[kHashSize], hslot[kPageMaxRows];
+  __shared__ uint64_t wsum[kPlanWaves];
+  __shared__ int wides;
+  constexpr int STEPS = 16;
+  int v[STEPS];   // counts of the first pages, on their way while the rows are looked at
+  auto load_counts = [&](int base) {
+    const int p0 = base + (threadIdx.x >> 6) * 64 * STEPS + (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) v[i] = p0 + 64 * i < np ? a.refs[p0 + 64 * i] : 1;
+  };
+  load_counts(0);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i < kHashSize; i += kPlanThreads) {
+  // (a hash table for the rows there are: at least twice as many slots)
+  const int bits = imax(6, 33 - __clz(imax(1, a.rows - 1)));
+  for (int i = tid; i < 1 << bits; i += kPlanThreads) {
     hkey[i] = -1;
     hcount[i] = 0;
     hlow[i] = INT_MAX;
   }
+  if (tid == 0) wides = 0;
   __syncthreads();
   const ReservePlan pl = reserve_plan(a.scratch, a.rows);
-  int len[kPlanRows], add[kPlanRows], last[kPlanRows], slot[kPlanRows], refs[kPlanRows];
-  bool lost[kPlanRows];   // the part-filled last page's entry names no page
-  int wide = 0;
-#pragma unroll
-  for (int k = 0; k < kPlanRows; ++k) {
-    const int r = tid * kPlanRows + k;
-    len[k] = add[k] = 0;
-    slot[k] = last[k] = -1;
-    lost[k] = false;
-    if (r >= a.rows) continue;
-    len[k] = clamp_len(a.lens[r], mp, shift);
-    add[k] = imax(0, a.n_add ? a.n_add[r] : a.n_add_all);
-    if (add[k] > (mp << shift) - len[k]) {
-      ++wide;
-      add[k] = (mp << shift) - len[k];
+  struct Row {
+    int len, add, last, refs;   // tokens, granted at best, part-filled last page (-1: none, or lost) and its count
+    bool wide, lost;            // past the table; the part-filled last page's entry names no page
+  };
+  auto row = [&](int r) {
+    Row w;
+    w.len = clamp_len(a.lens[r], mp, shift);
+    w.add = imax(0, a.n_add ? a.n_add[r] : a.n_add_all);
+    const int room = (mp << shift) - w.len;
+    w.wide = w.add > room;
+    w.add = imin(w.add, room);
+    w.last = -1;
+    w.refs = 0;
+    w.lost = false;
+    if (w.add > 0 && (w.len & mask) != 0) {
+      w.last = a.table[(int64_t)r * mp + pages_of(w.len, shift) - 1];
+      w.lost = !is_page(w.last, np);
+      if (w.lost) w.last = -1;
+      else w.refs = a.refs[w.last];
     }
-    if (add[k] == 0 || (len[k] & mask) == 0) continue;
-    last[k] = a.table[(int64_t)r * mp + pages_of(len[k], shift) - 1];
-    lost[k] = !is_page(last[k], np);
-    refs[k] = lost[k] ? 0 : a.refs[last[k]];
-    if (refs[k] < 2) continue;
-    int h = (int)(((uint32_t)last[k] * 2654435761u) >> (32 - kHashBits));
-    for (;; h = (h + 1) & (kHashSize - 1)) {
-      const int was = atomicCAS(&hkey[h], -1, last[k]);
-      if (was == -1 || was == last[k]) break;
+    return w;
+  };
+  Row first_row;   // of this thread's rows, the only one below 1024 rows
+  for (int r = tid; r < a.rows; r += kPlanThreads) {
+    const Row w = row(r);
+    if (r == tid) first_row = w;
+    if (w.wide) atomicAdd(&wides, 1);
+    hslot[r] = -1;
+    if (w.refs < 2) continue;
+    int h = (int)(((uint32_t)w.last * 2654435761u) >> (32 - bits));
+    for (;; h = (h + 1) & ((1 << bits) - 1)) {
+      const int was = atomicCAS(&hkey[h], -1, w.last);
+      if (was == -1 || was == w.last) break;
     }
-    slot[k] = h;
+    hslot[r] = h;
     atomicAdd(&hcount[h], 1);
     atomicMin(&hlow[h], r);
   }
   __syncthreads();
-  int need[kPlanRows], nneed = 0, ncopy = 0;
-  bool copy[kPlanRows];
-#pragma unroll
-  for (int k = 0; k < kPlanRows; ++k) {
-    const int r = tid * kPlanRows + k;
-    copy[k] = slot[k] >= 0 && !(hcount[slot[k]] == refs[k] && hlow[slot[k]] == r);
-    need[k] = pages_of(len[k] + add[k], shift) - pages_of(len[k], shift) + (copy[k] || lost[k] ? 1 : 0);
-    nneed += need[k];
-    ncopy += copy[k] ? 1 : 0;
+  int total = 0, copies = 0;
+  for (int base = 0; base < a.rows; base += kPlanThreads) {
+    const int r = base + tid;
+    int2 need = make_int2(0, 0);
+    Row w{0, 0, -1, 0, false, false};
+    bool copy = false;
+    if (r < a.rows) {
+      w = base == 0 ? first_row : row(r);
+      const int h = hslot[r];
+      copy = h >= 0 && !(hcount[h] == w.refs && hlow[h] == r);
+      need.x = pages_of(w.len + w.add, shift) - pages_of(w.len, shift) + (copy || w.lost ? 1 : 0);
+      need.y = copy ? 1 : 0;
+    }
+    int2 sum;
+    const int2 before = plan_scan2(need, wsum, &sum);
+    if (r < a.rows) {
+      pl.start[r] = pages_of(w.len, shift) - (copy || w.lost ? 1 : 0);
+      pl.need[r] = need.x;
+      pl.first[r] = total + before.x;
+      pl.len[r] = w.len;
+      pl.add[r] = w.add;
+      if (copy) {
+        const int pair = copies + before.y;
+        pl.src[pair] = w.last;
+        pl.at[pair] = total + before.x;
+        pl.part[pair] = w.len & mask;
+      }
+    }
+    total += sum.x;
+    copies += sum.y;
   }
-  int total, copies, wides;
-  int first = plan_scan(nneed, wsum, &total);
-  int pair = plan_scan(ncopy, wsum, &copies);
-  plan_scan(wide, wsum, &wides);
   // The lowest free pages, 64 KB of counts at a time: a wave takes 1024
   // consecutive ones.
-  constexpr int STEPS = 16;
   int found = 0;
   for (int base = 0; base < np && found < total; base += kPlanThreads * STEPS) {
     const int p0 = base + wave * 64 * STEPS + lane;
     uint64_t bits[STEPS];
     int n = 0;
-    int v[STEPS];
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) v[i] = p0 + 64 * i < np ? a.refs[p0 + 64 * i] : 1;
+    if (base > 0) load_counts(base);
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       bits[i] = __ballot(v[i] == 0);
       n += __popcll(bits[i]);
     }
-    int tot;
-    int at = found + __shfl(plan_scan(lane == 0 ? n : 0, wsum, &tot), 0, 64);
+    int2 tot;
+    int at = found + __shfl(plan_scan2(make_int2(lane == 0 ? n : 0, 0), wsum, &tot).x, 0, 64);
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int rank = at + __popcll(bits[i] & ((1ull << lane) - 1));
       if (v[i] == 0 && rank < total) pl.free[rank] = p0 + 64 * i;
       at += __popcll(bits[i]);
     }
-    found += tot;
+    found += tot.x;
   }
   const int missing = imax(0, total - found);
   const bool ok = missing == 0 && wides == 0;
-#pragma unroll
-  for (int k = 0; k < kPlanRows; ++k) {
-    const int r = tid * kPlanRows + k;
-    if (r >= a.rows) continue;
-    const int got = ok ? add[k] : 0;
-    pl.start[r] = pages_of(len[k], shift) - (copy[k] || lost[k] ? 1 : 0);
-    pl.need[r] = ok ? need[k] : 0;
-    pl.first[r] = first;
-    pl.new_len[r] = len[k] + got;
-    a.granted[r] = got;
-    if (copy[k]) {
-      pl.src[pair] = last[k];
-      pl.at[pair] = first;
-      pl.part[pair] = len[k] & mask;
-      ++pair;
-    }
-    first += need[k];
-  }
   if (tid == 0) {
     a.info[0] = missing;
     a.info[1] = wides;
@@ -260,14 +354,19 @@ __global__ void __launch_bounds__(256) reserve_apply_kernel(PageReserveArgs a) {
   const ReservePlan pl = reserve_plan(a.scratch, a.rows);
   const int lane = threadIdx.x & 63;
   const int w0 = blockIdx.x * 4 + (threadIdx.x >> 6), nw = gridDim.x * 4;
+  const bool ok = a.info[0] == 0 && a.info[1] == 0;
   for (int r = w0; r < a.rows; r += nw) {
-    const int need = pl.need[r], first = pl.first[r], start = pl.start[r];
+    const int need = ok ? pl.need[r] : 0, first = pl.first[r], start = pl.start[r];
     for (int k = lane; k < need; k += 64) {
       const int pg = pl.free[first + k];
       a.table_out[(int64_t)r * a.max_pages + start + k] = pg;
       a.refs_out[pg] = 1;
     }
-    if (lane == 0) a.lens_out[r] = pl.new_len[r];
+    if (lane == 0) {
+      const int got = ok ? pl.add[r] : 0;
+      a.granted[r] = got;
+      a.lens_out[r] = pl.len[r] + got;
+    }
   }
   const int copies = a.info[3];
   for (int i = w0 * 64 + lane; i < copies; i += nw * 64) atomicSub(&a.refs_out[pl.src[i]], 1);

@@ -38,7 +38,8 @@ def counts(table, lens, pt, n_pages):
 
 
 @pytest.mark.parametrize("rows,mp,pt,n_pages,new", [(1, 1, 16, 1, 1), (5, 3, 16, 40, 9), (17, 8, 32, 300, 40),
-                                                    (64, 21, 64, 1500, 33), (3, 5, 256, 20, 0), (300, 11, 128, 4000, 600)])
+                                                    (64, 21, 64, 1500, 33), (3, 5, 256, 20, 0), (300, 11, 128, 4000, 600),
+                                                    (200, 300, 16, 50000, 130), (900, 40, 16, 16384, 1000), (7, 3, 32, 16385, 0)])
 def test_fork(rows, mp, pt, n_pages, new):
     torch, sr = need_gpu()
     rng = np.random.default_rng(rows)
