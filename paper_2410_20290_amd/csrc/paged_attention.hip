@@ -203,7 +203,7 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 // Bound by memory: each key and value byte is read once.
 template <int HD, int NW>
 __global__ void __launch_bounds__(64 * NW)
-paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slot0, int slots, float qscale) {
+paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
   constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
   constexpr int KPD = 64 / CPK, NV = 32 / KPD;     // keys per V copy, copies of a block
   constexpr int INFLIGHT = 2 * KS + NV;            // memory operations of a block
@@ -402,46 +402,73 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     }
   }
 
-  // join the waves: per column (max, sum, unnormalised output)
+  // join the waves: per column the unnormalised output, (max, sum) behind it
+  constexpr int ROW = HD + 4;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   __syncthreads();
-  float* sm = reinterpret_cast<float*>(lds);   // [NW][16][HD + 2]
-  float* w = sm + (wave * 16 + fr) * (HD + 2);
+  float* sm = reinterpret_cast<float*>(lds);   // [NW][16][ROW]
+  float* w = sm + (wave * 16 + fr) * ROW;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[dt * 16 + 4 * fg + i] = o[dt][i];
+  for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(w + dt * 16 + 4 * fg) = o[dt];
   if (fg == 0) {
     w[HD] = m;
     w[HD + 1] = l;
   }
   __syncthreads();
+  // A thread takes eight dimensions of a column.  With one split the shared keys'
+  // slots are joined here too (up to FOLD at a time) and the output is written.
+  constexpr int FOLD = 4;
   const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, slots};
-  for (int i = threadIdx.x; i < rs.n * g * HD; i += 64 * NW) {
-    const int x = i / HD, d = i % HD;
-    float M = -INFINITY;
+  for (int i = threadIdx.x; i < rs.n * g * CPK; i += 64 * NW) {
+    const int x = i / CPK, d = 8 * (i % CPK);
+    const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
+    float M = -INFINITY, L = 0.f, A[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m1, float l1, const float* o8) {
+      if (m1 == -INFINITY) return;
+      const float mn = fmaxf(M, m1), ca = __builtin_amdgcn_exp2f(M - mn), cb = __builtin_amdgcn_exp2f(m1 - mn);
+      M = mn;
+      L = L * ca + l1 * cb;
 #pragma unroll
-    for (int k = 0; k < NW; ++k) M = fmaxf(M, sm[(k * 16 + x) * (HD + 2) + HD]);
-    float L = 0.f, A = 0.f;
-    if (M != -INFINITY) {
+      for (int e = 0; e < 8; ++e) A[e] = A[e] * ca + o8[e] * cb;
+    };
+    if (splits == 1) {
+      for (int k0 = 0; k0 < pre; k0 += FOLD) {
+        float2 ml[FOLD];
+        float4 v[FOLD][2];
 #pragma unroll
-      for (int k = 0; k < NW; ++k) {
-        const float* ws = sm + (k * 16 + x) * (HD + 2);
-        const float c = __builtin_amdgcn_exp2f(ws[HD] - M);
-        L += ws[HD + 1] * c;
-        A += ws[d] * c;
+        for (int k = 0; k < FOLD; ++k) {
+          const int slot = imin(k0 + k, pre - 1);
+          ml[k] = *reinterpret_cast<const float2*>(pt.ml(th, slot, HD));
+          const float4* src = reinterpret_cast<const float4*>(pt.o(th, slot, HD) + d);
+          v[k][0] = src[0];
+          v[k][1] = src[1];
+        }
+#pragma unroll
+        for (int k = 0; k < FOLD; ++k) {
+          const float o8[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w, v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
+          if (k0 + k < pre) add(ml[k].x, ml[k].y, o8);
+        }
       }
     }
-    const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
-    if (slots == 1) {
-      ((bf16_t*)a.out)[th * HD + d] = f32_to_bf16(L > 0.f ? A / L : 0.f);
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const float* ws = sm + (k * 16 + x) * ROW;
+      const f32x4 u = *reinterpret_cast<const f32x4*>(ws + d), v = *reinterpret_cast<const f32x4*>(ws + d + 4);
+      const float o8[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+      add(ws[HD], ws[HD + 1], o8);
+    }
+    if (splits == 1) {
+      const float inv = L > 0.f ? 1.f / L : 0.f;
+      bf16x8 r;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = (__bf16)(A[e] * inv);
+      *reinterpret_cast<bf16x8*>((bf16_t*)a.out + th * HD + d) = r;
     } else {
-      pt.o(th, slot0 + split, HD)[d] = A;
-      if (d == 0) {
-        pt.ml(th, slot0 + split, HD)[0] = M;
-        pt.ml(th, slot0 + split, HD)[1] = L;
-      }
+      float4* dst = reinterpret_cast<float4*>(pt.o(th, pre + split, HD) + d);
+      dst[0] = make_float4(A[0], A[1], A[2], A[3]);
+      dst[1] = make_float4(A[4], A[5], A[6], A[7]);
+      if (d == 0) *reinterpret_cast<float2*>(pt.ml(th, pre + split, HD)) = make_float2(M, L);
     }
   }
 }
@@ -495,8 +522,7 @@ constexpr int kTileCols = 128;
 
 template <int HD, bool PRE>
 __global__ void __launch_bounds__(256, 2)
-paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slot0, int slots,
-                  float qscale) {
+paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slots, float qscale) {
   constexpr int KT = 32, NW = 4;
   constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
   constexpr int TILE = KT * HD;                // bf16 elements of a K (or V) block
@@ -864,12 +890,12 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     }
   }
   l += other_half(l);
-  if (slots > 1) {
+  if (PRE || slots > 1) {
     if (!live) return;
     const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, slots};
     const int x = xw + fr, tok = x / g;
     const int64_t th = (int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g);
-    float* po = pt.o(th, slot0 + split, HD);
+    float* po = pt.o(th, split, HD);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -877,7 +903,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
         *reinterpret_cast<float4*>(po + 32 * dt + 8 * q4 + 4 * fh) =
             make_float4(o[dt][4 * q4], o[dt][4 * q4 + 1], o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
     if (fh == 0) {
-      float* ml = pt.ml(th, slot0 + split, HD);
+      float* ml = pt.ml(th, split, HD);
       ml[0] = m;
       ml[1] = l;
     }
@@ -905,7 +931,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 }
 
 // ----------------------------------------------------------------- merge
-// A wave joins the slots of one (token, query head).
+// A wave joins the slots of one (token, query head): lane s weighs slots s and s
+// + 64, then every lane sums its dimensions over the slots.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int slots) {
   const int64_t th = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -914,18 +941,24 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
   const int token = (int)(th / a.hq), row = token / a.lr;
   if (token - row * a.lr >= row_state(a, row).n) return;
   const int lane = threadIdx.x & 63;
-  const float* ml = pt.ml(th, 0, HD);
-  float M = -INFINITY;
-  for (int s = 0; s < slots; ++s) M = fmaxf(M, ml[2 * s]);
-  for (int d = lane; d < HD; d += 64) {
-    float L = 0.f, A = 0.f;
-    if (M != -INFINITY)
-      for (int s = 0; s < slots; ++s) {
-        const float c = exp2f(ml[2 * s] - M);
-        L += ml[2 * s + 1] * c;
-        A += pt.o(th, s, HD)[d] * c;
-      }
-    ((T*)a.out)[th * HD + d] = from_f32<T>(L > 0.f ? A / L : 0.f);
+  const float2* ml = reinterpret_cast<const float2*>(pt.ml(th, 0, HD));
+  const float2 none = make_float2(-INFINITY, 0.f);
+  const float2 x = lane < slots ? ml[lane] : none, y = lane + 64 < slots ? ml[lane + 64] : none;
+  const float M = wave_max(fmaxf(x.x, y.x));
+  const float ref = M == -INFINITY ? 0.f : M;
+  const float wx = __builtin_amdgcn_exp2f(x.x - ref), wy = __builtin_amdgcn_exp2f(y.x - ref);
+  const float L = wave_sum(x.y * wx + y.y * wy);
+  constexpr int N = HD < 64 ? 1 : HD / 64;   // dimensions of a lane
+  float A[N] = {};
+  if (N * lane < HD) {
+    const float* o = pt.o(th, 0, HD) + N * lane;
+    for (int s = 0; s < slots; ++s) {
+      const float w = __shfl(s < 64 ? wx : wy, s & 63, 64);
+#pragma unroll
+      for (int e = 0; e < N; ++e) A[e] += w * o[(int64_t)s * HD + e];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) ((T*)a.out)[th * HD + N * lane + e] = from_f32<T>(L > 0.f ? A[e] / L : 0.f);
   }
 }
 
@@ -936,7 +969,9 @@ struct PagedPlan {
   int nw;       // PAGED_WAVE: waves of a work-group
   int splits;   // work-groups that share a row's keys
   int pre;      // PAGED_WAVE: splits of the shared keys' own pass (0: none)
-  int slots() const { return splits + pre; }   // partial slots (1: the pass writes the output)
+  // Partial slots: the shared keys' first, then the row's own splits (none where
+  // one work-group takes them all: it writes the output).
+  int slots() const { return pre + (splits > 1 ? splits : 0); }
 };
 
 // Query heads of a work-group of the vector kernel.
@@ -995,7 +1030,7 @@ static PagedPlan paged_plan(const PagedAttnArgs& a) {
 
 // Scratch: the partial slots, then common[rows].
 static size_t partial_floats(const PagedAttnArgs& a, const PagedPlan& p) {
-  return p.slots() > 1 ? (size_t)a.rows * a.lr * a.hq * p.slots() * (a.hd + 2) : 0;
+  return (size_t)a.rows * a.lr * a.hq * p.slots() * (a.hd + 2);
 }
 size_t paged_attn_scratch(const PagedAttnArgs& a) {
   if (a.rows <= 0 || a.lr <= 0) return 0;
@@ -1039,7 +1074,7 @@ static void launch_tile(const PagedAttnArgs& a, const int32_t* common, int split
   const int64_t cols = (int64_t)(PRE ? a.rows : 1) * a.lr * (a.hq / a.hkv);
   const int64_t total = (cols + kTileCols - 1) / kTileCols * splits * a.hkv * (PRE ? 1 : a.rows);
   SR_REQUIRE(total <= (int64_t)INT_MAX - 8, SR_ERR_UNSUPPORTED, "attention grid too large");
-  SR_LAUNCH((paged_tile_kernel<HD, PRE>), dim3((unsigned)(8 * ((total + 7) / 8))), dim3(256), 0, s, a, common, splits, 0,
+  SR_LAUNCH((paged_tile_kernel<HD, PRE>), dim3((unsigned)(8 * ((total + 7) / 8))), dim3(256), 0, s, a, common, splits,
             slots, qscale);
   SR_CHECK_LAUNCH();
 }
@@ -1066,7 +1101,7 @@ static void launch_wave(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t 
   }
 #undef SR_PAGED_WAVE
   SR_CHECK_LAUNCH();
-  if (p.slots() > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
+  if (p.splits > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
 }
 
 template <int HD>
@@ -1076,7 +1111,7 @@ static void matrix_cores(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t
     return;
   }
   launch_tile<HD, false>(a, nullptr, p.splits, p.slots(), s);
-  if (p.slots() > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
+  if (p.splits > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
 }
 
 void paged_attn(const PagedAttnArgs& a, hipStream_t s) {
