@@ -516,12 +516,12 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // block are formed under the probabilities of this one; 16-byte chunks sit
 // XOR-swizzled in the LDS rows.  Two work-groups a CU.  With several splits a
 // work-group takes an even share of the blocks.
-constexpr int kTileStages = 4;
+constexpr int kTileStages = 3;
 constexpr float kStale = 8.f;
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, 3)
 paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slots, float qscale) {
   constexpr int KT = 32, NW = 4;
   constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
@@ -724,16 +724,14 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   // LDS element offsets: the K fragment of key fr (chunk 2 s + fh), and the
   // four dims dt 32 + 16 (l / 16 % 2) + 4 (l % 4) .. of V key 4 fh + l % 16 / 4
   bf16x8 qf[KS];
-  int koff[KS];
-  uint32_t vbase[DT];   // LDS bytes, in the first stage's V block
-#pragma unroll
-  for (int s = 0; s < KS; ++s) koff[s] = fr * HD + 8 * ((2 * s + fh) ^ (fr & (CPK - 1)));
+  // byte offset in a stage of chunk fh of K row fr (chunk 2 s + fh: this ^ 32 s)
+  const uint32_t kbase = (uint32_t)(fr * HD + 8 * (fh ^ (fr & (CPK - 1)))) * 2;
+  // LDS address in the first V block of dims 16 (l / 16 % 2) + 4 (l % 4) .. of key
+  // 4 fh + l % 16 / 4 (dims 32 dt on: this ^ 64 dt)
+  uint32_t vbase;
   {
     const int vk = 4 * fh + ((lane & 15) >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      vbase[dt] = lds_addr(lds + TILE + vk * HD +
-                           8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vswz(vk)) + 4 * (lane & 1));
+    vbase = lds_addr(lds + TILE + vk * HD + 8 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vswz(vk)) + 4 * (lane & 1));
   }
 
   f32x16 o[DT];
@@ -756,52 +754,19 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
     return fmaxf(mt, other_half(mt));
   };
-  // Block `tile` in stage ST: its scores `sc`, their maxima mt (before masking)
-  // and the V of its first 16 keys (lo, hi) are there; the scores of the next
-  // block are formed into `sn`.  Per 16-key chunk every score product runs beside
-  // a share of the chunk's probabilities; K and the second chunk's V are read
-  // under the products before their use, the next block's first V and its scores'
-  // maxima under the last ones.
-  constexpr int KC = KS / 2;     // score products of a chunk
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
-  i16x4 lo[DT], hi[DT];
-  float mt = -INFINITY;
-  auto step = [&](auto stage, int tile, uint32_t f, f32x16& sc, f32x16& sn) {
-    constexpr int ST = decltype(stage)::value, NX = (ST + 1) % kTileStages;
-    constexpr int VB = ST * 2 * TILE * 2, VN = NX * 2 * TILE * 2;   // bytes from vbase
-    bf16x8 kf[KC], pf;
-    auto read_k = [&](int c) {
+  auto frag = [&](const bf16_t* base, int s) {
+    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(base) + (kbase ^ (32u * s)));
+  };
+  auto step = [&](auto stage, int tile, uint32_t f) {
+    constexpr int ST = decltype(stage)::value;
+    constexpr int VB = ST * 2 * TILE * 2;   // bytes from vbase
+    f32x16 sc;
+    zero(sc);
 #pragma unroll
-      for (int s = 0; s < KC; ++s)
-        kf[s] = *reinterpret_cast<const bf16x8*>(lds + (koff[c * KC + s] + NX * 2 * TILE));
-    };
-    auto scores = [&](int c) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s = 0; s < KC; ++s) {
-        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[c * KC + s], sn, 0, 0, 0);
-#pragma unroll
-        for (int e = s * 8 / KC; e < (s + 1) * 8 / KC; ++e) pf[e] = (__bf16)__builtin_amdgcn_exp2f(sc[8 * c + e] - m);
-      }
-      // (of the rounded ones, as the product has them)
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[e], pf[e + 1]}, ones, l, false);
-#pragma unroll
-      for (int s = 0; s < KC; ++s) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 8 / KC, 0);
-        __builtin_amdgcn_sched_group_barrier(0x400, 8 / KC, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 8 / KC, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto output = [&] {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf, o[dt], 0, 0, 0);
-    };
-    read_k(0);
+    for (int s = 0; s < KS; ++s)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(lds + ST * 2 * TILE, s), qf[s], sc, 0, 0, 0);
     if (f & EDGE) {                            // (uniform)
       asm volatile("");                        // (a branch, not selects on every block)
       // bit j: this lane's key j of the block (of the 32 from 4 fh on) is seen
@@ -812,8 +777,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       if (f & GONE1) seen &= 0x0000FFFFu;
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e] = (int)(seen << (31 - 8 * (e >> 2) - (e & 3))) < 0 ? sc[e] : -INFINITY;
-      mt = peak(sc);
     }
+    const float mt = peak(sc);
     // Probabilities are relative to a maximum up to 2^kStale out of date: a
     // rescaling of the accumulators costs as much as half a block's
     // exponentials, and a wave's 32 columns would need one in most blocks.
@@ -825,34 +790,33 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       for (int dt = 0; dt < DT; ++dt) o[dt] *= corr;
       m = mn;
     }
-    zero(sn);
-    scores(0);
-    read_k(1);
-    output();
+    uint32_t va[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) va[dt] = vbase ^ (64u * dt);
+    bf16x8 pf[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[c][e] = (__bf16)__builtin_amdgcn_exp2f(sc[8 * c + e] - m);
+      // (of the rounded ones, as the product has them)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[c][e], pf[c][e + 1]}, ones, l, false);
+    }
+    i16x4 lo[DT], hi[DT];
+    lds_read_tr16_pairs<DT, VB, VB + 8 * HD * 2>(va, lo, hi);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf[0], o[dt], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    lds_read_tr16_pairs<DT, VB + 16 * HD * 2, VB + 24 * HD * 2>(vbase, lo, hi);
-    scores(1);
-    output();
-    mt = peak(sn);
-    __builtin_amdgcn_sched_barrier(0);
-    lds_read_tr16_pairs<DT, VN, VN + 8 * HD * 2>(vbase, lo, hi);
-  };
-  // Before block i: block i + 1 landed too (its first scores are formed under
-  // block i; only the copies of i + 2 may still fly), and every wave is done
-  // with block i - 1, whose buffer takes block i + 3.
-  auto sync = [&](int tile, int next) {
-    if (tile + 2 < ntile) wait_barrier(std::integral_constant<int, CPW>{});
-    else wait_barrier(std::integral_constant<int, 0>{});
-    if (tile + kTileStages - 1 < ntile) issue(tile + kTileStages - 1, next);
+    lds_read_tr16_pairs<DT, VB + 16 * HD * 2, VB + 24 * HD * 2>(va, lo, hi);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr16_pair(lo[dt], hi[dt]), pf[1], o[dt], 0, 0, 0);
   };
   bf16_t* const slice = lds + wave * 32 * HD;
   if (ntile > 0) {
-    // Blocks 0 and 1 go out first; the scaled bf16 queries pass through the
-    // buffers of blocks 2 and 3 (a 32-row slice per wave, chunks placed like
-    // K's) into fragments: lane holds Q[column fr][16 s + 8 fh .. + 8].
     issue(0, 0);
-    if (ntile > 1) issue(1, 1);
-    bf16_t* qs = slice + 2 * 2 * TILE;
+    bf16_t* qs = slice + 2 * TILE;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
@@ -861,32 +825,21 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       *reinterpret_cast<bf16x4*>(qs + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
     }
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qs + koff[s]);
-    f32x16 sa, sb;
-    zero(sa);
-    wait_barrier(std::integral_constant<int, 0>{});   // blocks 0 and 1, and every wave's queries read
-    if (ntile > 2) issue(2, 2);
-    if (ntile > 3) issue(3, 3);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds + koff[s]);
-      sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sa, 0, 0, 0);
-    }
-    mt = peak(sa);
-    lds_read_tr16_pairs<DT, 0, 8 * HD * 2>(vbase, lo, hi);
-    // four blocks a round, a stage each; the scores formed past the last block
-    // are those of a stale buffer and never used
-    auto one = [&](auto stage, int tile, f32x16& sc, f32x16& sn) {
+    for (int s = 0; s < KS; ++s) qf[s] = frag(qs, s);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // every wave's queries read
+    if (ntile > 1) issue(1, 1);
+    auto one = [&](auto stage, int tile) {
       constexpr int ST = decltype(stage)::value;
-      if (tile > 0) sync(tile, (ST + kTileStages - 1) % kTileStages);
+      if (tile + 1 < ntile) wait_barrier(std::integral_constant<int, CPW>{});
+      else wait_barrier(std::integral_constant<int, 0>{});
+      if (tile + 2 < ntile) issue(tile + 2, (ST + 2) % kTileStages);
       const uint32_t f = ring >> (4 * ST);
-      if (!(f & PAST)) step(stage, tile, f, sc, sn);
+      if (!(f & PAST)) step(stage, tile, f);
     };
-    for (int tile = 0; tile < ntile; tile += 4) {
-      one(std::integral_constant<int, 0>{}, tile, sa, sb);
-      if (tile + 1 < ntile) one(std::integral_constant<int, 1>{}, tile + 1, sb, sa);
-      if (tile + 2 < ntile) one(std::integral_constant<int, 2>{}, tile + 2, sa, sb);
-      if (tile + 3 < ntile) one(std::integral_constant<int, 3>{}, tile + 3, sb, sa);
+    for (int tile = 0; tile < ntile; tile += 3) {
+      one(std::integral_constant<int, 0>{}, tile);
+      if (tile + 1 < ntile) one(std::integral_constant<int, 1>{}, tile + 1);
+      if (tile + 2 < ntile) one(std::integral_constant<int, 2>{}, tile + 2);
     }
   }
   l += other_half(l);
