@@ -53,10 +53,13 @@ struct Partials {
 };
 
 // ------------------------------------------------------------ vector ALU
-// Work-group = (split of the visible keys, GC query heads of one KV head,
-// token).  HD / 4 lanes share a key (four dimensions each), so a work-group
-// has 1024 / HD groups of lanes, each with a softmax state of its own; a group
-// has U keys in flight.  The groups are joined through LDS.
+// Work-group = (split of the visible keys, GC query columns of one row, KV head);
+// column x is token x / G, query head x % G as below.  HD / 4 lanes share a key
+// (four dimensions each), so a work-group has 1024 / HD groups of lanes, each
+// with a softmax state of its own per column; a group has U keys in flight, each
+// read once for all its columns.  The groups are joined through LDS.
+// Bound by instructions: 4 FMAs, log2(HD / 4) DPP adds and an exponential per key
+// and column and lane.
 template <typename T>
 __device__ __forceinline__ float4 load4(const T* p);
 template <>
@@ -70,104 +73,136 @@ __device__ __forceinline__ float4 load4<bf16_t>(const bf16_t* p) {
                      __uint_as_float(u.y & 0xFFFF0000u));
 }
 
+// The sum over aligned groups of LPK lanes, in every lane of a group: DPP moves
+// within rows of 16 (quads by xor 1 and 2, then mirrored halves, which by then
+// hold equal sums), a cross-lane move beyond.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int LPK>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v = dpp_add<0xB1>(v);                         // quad_perm [1,0,3,2]
+  v = dpp_add<0x4E>(v);                         // quad_perm [2,3,0,1]
+  v = dpp_add<0x141>(v);                        // row_half_mirror
+  if constexpr (LPK >= 16) v = dpp_add<0x140>(v);   // row_mirror
+  if constexpr (LPK == 32) v += __shfl_xor(v, 16, 64);
+  static_assert(LPK == 8 || LPK == 16 || LPK == 32, "lanes of a key");
+  return v;
+}
+
 template <typename T, int HD, int GC>
-__global__ void __launch_bounds__(256) paged_vector_kernel(PagedAttnArgs a, int splits, float qscale) {
+__global__ void __launch_bounds__(256, 2) paged_vector_kernel(PagedAttnArgs a, int splits, float qscale) {
   constexpr int LPK = HD / 4, NG = 256 / LPK, U = 4;
   __shared__ float sm[NG][GC][HD + 2];
-  const int split = blockIdx.x % splits, token = blockIdx.x / splits;
-  const int row = token / a.lr, t = token - row * a.lr;
+  const int g = a.hq / a.hkv, tiles = (a.lr * g + GC - 1) / GC;
+  const int split = blockIdx.x % splits, tile = blockIdx.x / splits, h = blockIdx.y;
+  const int row = tile / tiles, x0 = (tile - row * tiles) * GC;
   const RowState rs = row_state(a, row);
-  if (t >= rs.n) return;
-  const int qh0 = blockIdx.y * GC, h = qh0 / (a.hq / a.hkv);
-  const int p = rs.p0 + t, lo = window_start(p, a.window), sinks = imin(a.sinks, lo);
-  const int seen = sinks + p + 1 - lo;                 // visible keys, in order
-  const int per = (seen + splits - 1) / splits;
-  const int v1 = imin(seen, (split + 1) * per);
+  const int X = rs.n * g;                        // the row's columns
+  if (x0 >= X) return;
   const int grp = threadIdx.x / LPK, d = 4 * (threadIdx.x % LPK);
   const T* kpool = (const T*)a.kpool;
   const T* vpool = (const T*)a.vpool;
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
+  const int first = rs.p0 + x0 / g, last = rs.p0 + imin(x0 + GC, X) / g - (imin(x0 + GC, X) % g == 0 ? 1 : 0);
+  // keys that some column sees: [0, sinks) and [lo, last], in this order
+  const int lo = window_start(first, a.window), sinks = imin(a.sinks, lo), all_lo = window_start(last, a.window);
+  const int seen = sinks + last + 1 - lo;
+  const int per = (seen + splits - 1) / splits;
+  const int v1 = imin(seen, (split + 1) * per);
   float4 q[GC];
-#pragma unroll
-  for (int g = 0; g < GC; ++g) {
-    q[g] = *reinterpret_cast<const float4*>(a.q + ((int64_t)token * a.hq + qh0 + g) * HD + d);
-    q[g].x *= qscale; q[g].y *= qscale; q[g].z *= qscale; q[g].w *= qscale;
-  }
+  int end[GC], from[GC];                         // column c sees keys below end[c] from from[c] on, and the sinks
   float m[GC], l[GC], acc[GC][4];
 #pragma unroll
-  for (int g = 0; g < GC; ++g) {
-    m[g] = -INFINITY;
-    l[g] = 0.f;
+  for (int c = 0; c < GC; ++c) {
+    const int x = imin(x0 + c, X - 1), t = x / g;
+    end[c] = rs.p0 + t + 1;
+    from[c] = window_start(rs.p0 + t, a.window);
+    q[c] = *reinterpret_cast<const float4*>(a.q + (((int64_t)row * a.lr + t) * a.hq + h * g + (x - t * g)) * HD + d);
+    q[c].x *= qscale; q[c].y *= qscale; q[c].z *= qscale; q[c].w *= qscale;
+    m[c] = -INFINITY;
+    l[c] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[g][e] = 0.f;
+    for (int e = 0; e < 4; ++e) acc[c][e] = 0.f;
   }
   for (int v0 = split * per; v0 < v1; v0 += NG * U) {   // (uniform in the work-group)
     int64_t off[U];
+    int key[U];
     bool ok[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int v = v0 + u * NG + grp, vc = imin(v, v1 - 1);
-      const int j = vc < sinks ? vc : vc - sinks + lo;
-      const int pg = tab[j >> a.shift];
+      key[u] = vc < sinks ? vc : vc - sinks + lo;
+      const int pg = tab[key[u] >> a.shift];
       ok[u] = v < v1 && (uint32_t)pg < (uint32_t)a.n_pages;
-      off[u] = page_offset(ok[u] ? pg : 0, a.hkv, h, a.shift, j, HD) + d;
+      off[u] = page_offset(ok[u] ? pg : 0, a.hkv, h, a.shift, key[u], HD) + d;
     }
-    float4 k[U], x[U];
+    // some column does not see some of the keys
+    const int vlast = imin(v0 + NG * U, v1) - 1;
+    const bool edge = (vlast < sinks ? vlast : vlast - sinks + lo) > first || (v0 - sinks + lo < all_lo && v0 >= sinks) ||
+                      (vlast >= sinks && v0 < sinks && lo < all_lo);
+    float4 k[U], y[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) k[u] = load4<T>(kpool + off[u]);
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = load4<T>(vpool + off[u]);
+    for (int u = 0; u < U; ++u) y[u] = load4<T>(vpool + off[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (!ok[u]) x[u] = make_float4(0.f, 0.f, 0.f, 0.f);   // (what lies there may be no number)
+      if (!ok[u]) y[u] = make_float4(0.f, 0.f, 0.f, 0.f);   // (what lies there may be no number)
 #pragma unroll
-    for (int g = 0; g < GC; ++g) {
-      float s[U], mn = m[g];
+    for (int c = 0; c < GC; ++c) {
+      float s[U], mn = m[c];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        s[u] = lanes_sum<LPK>(q[c].x * k[u].x + q[c].y * k[u].y + q[c].z * k[u].z + q[c].w * k[u].w);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        s[u] = q[g].x * k[u].x + q[g].y * k[u].y + q[g].z * k[u].z + q[g].w * k[u].w;
-#pragma unroll
-        for (int o = LPK / 2; o > 0; o >>= 1) s[u] += __shfl_xor(s[u], o, 64);
-        if (!ok[u]) s[u] = -INFINITY;
+        bool sees = ok[u];
+        if (edge) sees = sees & (key[u] < end[c]) & ((key[u] >= from[c]) | (key[u] < a.sinks));
+        if (!sees) s[u] = -INFINITY;
         mn = fmaxf(mn, s[u]);
       }
       const float ref = mn == -INFINITY ? 0.f : mn;
-      const float corr = exp2f(m[g] - ref);   // (0 while nothing was seen)
-      m[g] = mn;
-      l[g] *= corr;
+      const float corr = __builtin_amdgcn_exp2f(m[c] - ref);   // (0 while nothing was seen)
+      m[c] = mn;
+      l[c] *= corr;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[g][e] *= corr;
+      for (int e = 0; e < 4; ++e) acc[c][e] *= corr;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float w = exp2f(s[u] - ref);
-        l[g] += w;
-        acc[g][0] += w * x[u].x; acc[g][1] += w * x[u].y; acc[g][2] += w * x[u].z; acc[g][3] += w * x[u].w;
+        const float w = __builtin_amdgcn_exp2f(s[u] - ref);
+        l[c] += w;
+        acc[c][0] += w * y[u].x; acc[c][1] += w * y[u].y; acc[c][2] += w * y[u].z; acc[c][3] += w * y[u].w;
       }
     }
   }
 #pragma unroll
-  for (int g = 0; g < GC; ++g) {
+  for (int c = 0; c < GC; ++c) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sm[grp][g][d + e] = acc[g][e];
+    for (int e = 0; e < 4; ++e) sm[grp][c][d + e] = acc[c][e];
     if (d == 0) {
-      sm[grp][g][HD] = m[g];
-      sm[grp][g][HD + 1] = l[g];
+      sm[grp][c][HD] = m[c];
+      sm[grp][c][HD + 1] = l[c];
     }
   }
   __syncthreads();
   const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, splits};
   for (int i = threadIdx.x; i < GC * HD; i += 256) {
-    const int g = i / HD, dd = i % HD;
+    const int c = i / HD, dd = i % HD, x = x0 + c;
+    if (x >= X) break;
     float M = -INFINITY;
-    for (int k = 0; k < NG; ++k) M = fmaxf(M, sm[k][g][HD]);
+#pragma unroll 8
+    for (int k = 0; k < NG; ++k) M = fmaxf(M, sm[k][c][HD]);
     float L = 0.f, A = 0.f;
     if (M != -INFINITY)
+#pragma unroll 8
       for (int k = 0; k < NG; ++k) {
-        const float c = exp2f(sm[k][g][HD] - M);
-        L += sm[k][g][HD + 1] * c;
-        A += sm[k][g][dd] * c;
+        const float w = __builtin_amdgcn_exp2f(sm[k][c][HD] - M);
+        L += sm[k][c][HD + 1] * w;
+        A += sm[k][c][dd] * w;
       }
-    const int64_t th = (int64_t)token * a.hq + qh0 + g;
+    const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
     if (splits == 1) {
       ((T*)a.out)[th * HD + dd] = from_f32<T>(L > 0.f ? A / L : 0.f);
     } else {
@@ -943,8 +978,12 @@ struct PagedPlan {
   int slots() const { return pre + (splits > 1 ? splits : 0); }
 };
 
-// Query heads of a work-group of the vector kernel.
-static int vector_heads(int g) { return g % 4 == 0 ? 4 : g % 2 == 0 ? 2 : 1; }
+// Query columns of a work-group of the vector kernel, for rows of `cols` of them.
+static int vector_cols(int cols) { return cols >= 8 ? 8 : cols >= 4 ? 4 : cols >= 2 ? 2 : 1; }
+static int64_t vector_groups(const PagedAttnArgs& a) {
+  const int cols = a.lr * (a.hq / a.hkv), gc = vector_cols(cols);
+  return (int64_t)a.rows * a.hkv * ((cols + gc - 1) / gc);
+}
 
 // Keys that a row's queries see at most, as far as the host knows.
 static int64_t planned_keys(const PagedAttnArgs& a) {
@@ -991,7 +1030,7 @@ static PagedPlan paged_plan(const PagedAttnArgs& a) {
     const int64_t tiles = ((int64_t)a.lr * g + kTileCols - 1) / kTileCols;
     p.splits = tile_splits(tiles * a.hkv * a.rows, keys / 32);
   } else {
-    const int64_t groups = (int64_t)a.rows * a.lr * (a.hq / vector_heads(g));
+    const int64_t groups = vector_groups(a);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, keys / 256, kMaxSplits}));
   }
   return p;
@@ -1017,13 +1056,17 @@ static void launch_merge(const PagedAttnArgs& a, int slots, hipStream_t s) {
 template <typename T, int HD>
 static void launch_vector(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
-  const int gc = vector_heads(a.hq / a.hkv);
-  const dim3 grid((unsigned)((int64_t)a.rows * a.lr * p.splits), a.hq / gc);
-  switch (gc) {
-    case 4: SR_LAUNCH((paged_vector_kernel<T, HD, 4>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
-    case 2: SR_LAUNCH((paged_vector_kernel<T, HD, 2>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
-    default: SR_LAUNCH((paged_vector_kernel<T, HD, 1>), grid, dim3(256), 0, s, a, p.splits, qscale); break;
+  const int64_t blocks = vector_groups(a) / a.hkv * p.splits;
+  SR_REQUIRE(blocks <= INT_MAX, SR_ERR_UNSUPPORTED, "attention grid too large");
+  const dim3 grid((unsigned)blocks, a.hkv);
+#define SR_VECTOR(GC) SR_LAUNCH((paged_vector_kernel<T, HD, GC>), grid, dim3(256), 0, s, a, p.splits, qscale)
+  switch (vector_cols(a.lr * (a.hq / a.hkv))) {
+    case 8: SR_VECTOR(8); break;
+    case 4: SR_VECTOR(4); break;
+    case 2: SR_VECTOR(2); break;
+    default: SR_VECTOR(1); break;
   }
+#undef SR_VECTOR
   SR_CHECK_LAUNCH();
   if (p.splits > 1) launch_merge<T, HD>(a, p.splits, s);
 }
