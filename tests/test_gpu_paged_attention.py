@@ -133,6 +133,34 @@ def test_shared_prompt(bf16, hd, hq, hkv, rows):
     case(22, bf16, hd, hq, hkv, [0] + lens[1:], 1, 32, shared=0, shared_arg=160)  # row 0 has nothing
 
 
+SHARE = [(128, 4, 1, 700), (64, 2, 1, 1300), (128, 2, 2, 350), (64, 16, 1, 1250)]
+
+
+@pytest.mark.parametrize("hd,hq,hkv,rows", SHARE)
+def test_shared_prompt_in_a_pass_of_its_own(hd, hq, hkv, rows):
+    """Enough rows that the shared keys are attended once for all of them
+    (300 MB of reads saved): right, too long and partly wrong hints, rows that
+    leave the prompt early or lack it, windows that have left key 0, drafts."""
+    rng = np.random.default_rng(rows)
+    S = 1024
+    assert rows * S * hkv * hd * 4 >= 300 << 20
+    lens = (S + rng.integers(1, 40, rows)).tolist()
+    case(40, True, hd, hq, hkv, lens, 1, 64, shared=S)
+    case(41, True, hd, hq, hkv, lens, 1, 16, shared=S - 16, shared_arg=S + 777)      # an odd number of 16-token pages
+    mixed = list(lens)
+    for r in range(0, rows, 7):
+        mixed[r] = int(rng.integers(0, S))                                          # row 0 among them
+    mixed[0] = S - 70
+    case(42, True, hd, hq, hkv, mixed, 1, 32, shared=S)
+    holes = {(r, int(rng.integers(0, 32))): -1 for r in range(5, rows, 11)}
+    case(43, True, hd, hq, hkv, lens, 1, 32, shared=S, holes=holes)
+    case(44, True, hd, hq, hkv, lens, 1, 32, shared=S, holes={(0, 3): -1, (0, 9): 1 << 30})   # row 0's own pages are missing
+    case(45, True, hd, hq, hkv, [0] + lens[1:], 1, 32, shared=0, shared_arg=S)       # nothing in common with row 0
+    case(46, True, hd, hq, hkv, lens, 1, 32, window=S + 20, sinks=5, shared=S, max_len=S)   # some windows have left key 0
+    if 2 * hq // hkv <= 16:
+        case(47, True, hd, hq, hkv, lens, 2, 32, shared=S, n_new=[int(n) for n in rng.integers(0, 3, rows)])
+
+
 @pytest.mark.parametrize("bf16,hd,hq,hkv", [(True, 128, 8, 2), (True, 64, 4, 1), (False, 32, 4, 4)])
 def test_long_rows_split_over_work_groups(bf16, hd, hq, hkv):
     case(23, bf16, hd, hq, hkv, [5003], 1, 64)
@@ -185,14 +213,15 @@ def test_graph_replays_and_streams():
         sr.paged_attention(qd * 2, k, v, table, ln, torch.empty_like(out))
 
 
-def test_results_repeat_bit_for_bit():
+@pytest.mark.parametrize("rows,shared", [(80, 192), (700, 1024)])
+def test_results_repeat_bit_for_bit(rows, shared):
     torch, sr = need_gpu()
     rng = np.random.default_rng(30)
-    lens = (200 + rng.integers(1, 400, 80)).tolist()
-    cache = Cache(rng, lens, 32, 2, 128, True, shared=6)
-    cache.poison([1] * 80, 0, 0)
-    q = rng.normal(size=(80, 1, 8, 128)).astype(np.float32)
-    first, _ = run(torch, sr, cache, q, [1] * 80, 1, 0, 0, shared=192)
+    lens = (shared + rng.integers(1, 100, rows)).tolist()
+    cache = Cache(rng, lens, 32, 2, 128, True, shared=shared // 32)
+    cache.poison([1] * rows, 0, 0)
+    q = rng.normal(size=(rows, 1, 8, 128)).astype(np.float32)
+    first, _ = run(torch, sr, cache, q, [1] * rows, 1, 0, 0, shared=shared)
     for _ in range(3):
-        again, _ = run(torch, sr, cache, q, [1] * 80, 1, 0, 0, shared=192)
+        again, _ = run(torch, sr, cache, q, [1] * rows, 1, 0, 0, shared=shared)
         assert np.array_equal(first, again)
