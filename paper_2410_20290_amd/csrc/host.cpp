@@ -1036,7 +1036,12 @@ static sr_status guard(F&& f) {
   return (sr_status)guarded(f);
 }
 
-void set_last_error(const char* msg) { t_err = msg; }
+void set_last_error(const char* msg) {
+  try {
+    t_err = msg;
+  } catch (...) {   // (no memory for the message: the status still says what happened)
+  }
+}
 
 }  // namespace sr
 
