@@ -129,7 +129,7 @@ sr_status sr_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, do
  * q past n_new[r], and tokens whose entry names no page, are not written.
  * Two rows that write one page write it in no fixed order: reserve the tokens
  * first (sr_page_reserve).  rot_dim: 0 or a multiple of 8 up to head_dim;
- * head_dim in {32, 64, 128}; qkv, q 16-byte aligned. */
+ * head_dim in {32, 64, 128}; rows * lr < 2^24; qkv, q 16-byte aligned. */
 sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
                          int32_t rows, int32_t lr, const float *qkv, const double *freqs, int32_t rot_dim,
                          int32_t interleaved, void *kpool, void *vpool, int32_t page_tokens,
@@ -149,15 +149,20 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
  * entries that name no page) may hold anything, NaN included; a key or value
  * that one query sees and another query of the call does not must be finite.
  * shared: a number of leading tokens whose pages most rows have in common with
- * row 0 (a forked prompt).  Their part is computed once for all rows whose
- * entries equal row 0's, which is checked on the device: the result does not
- * depend on it beyond rounding.  Rows with lr tokens or fewer behind it gain
- * nothing.  max_len: the longest row the caller expects (plans the split of
- * the work over the keys; rows may be longer), >= 1.
- * head_dim in {32, 64, 128}; n_heads / n_kv_heads <= 16.  bf16 with head_dim
- * 64 or 128 runs on the matrix cores (queries and probabilities rounded to
- * bf16, sums in fp32).  q, kpool, vpool, out 16-byte aligned.  scratch:
- * DEVICE float of scratch_elems >= sr_paged_attention_scratch(...) elements. */
+ * row 0 (a forked prompt).  bf16 calls of at most 16 query columns a row (lr
+ * n_heads / n_kv_heads) compute their part once for all rows whose entries
+ * equal row 0's, which is checked on the device, where that saves 300 MB of
+ * reads or more; rows that name other pages, or whose window has left key 0,
+ * read their own.  The result does not depend on it beyond rounding.
+ * max_len: the longest row the caller expects (plans the split of the work over
+ * the keys; rows may be longer), >= 1.
+ * head_dim in {32, 64, 128}; n_heads / n_kv_heads <= 16; rows * lr * n_heads <=
+ * 2^28; calls of 2^24 work-groups (of 1 to 8 query columns, prompts in bf16 of
+ * 128) are refused.  bf16 with head_dim 64 or 128 runs on the matrix cores:
+ * probabilities rounded to bf16, sums in fp32, queries in 16 bits where a row
+ * has at most 8 query columns, rounded to bf16 elsewhere and for the shared
+ * part.  q, kpool, vpool, out 16-byte aligned.  scratch: DEVICE float of
+ * scratch_elems >= sr_paged_attention_scratch(...) elements. */
 sr_status sr_paged_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
                              int32_t rows, int32_t lr, const float *q, const void *kpool,
                              const void *vpool, int32_t page_tokens, int32_t n_pages,
@@ -169,8 +174,8 @@ size_t sr_paged_attention_scratch(int32_t dtype, int32_t head_dim, int32_t n_hea
                                   int32_t rows, int32_t lr, int32_t page_tokens, int32_t max_pages,
                                   int32_t window, int32_t sinks, int32_t shared, int32_t max_len);
 
-/* Log-probabilities under softmax(logits[r] / temperature), the distribution
- * sr_sample draws from (temperature > 0), for every row r < rows of logits
+/* Log-probabilities under softmax(logits[r] / temperature) (temperature > 0; for
+ * finite logits the distribution that sr_sample draws from), for every row r < rows of logits
  * (DEVICE dtype [rows][row_stride], vocab <= row_stride entries used, vocab <=
  * 262144, rows <= 2^20).  Any output may be NULL:
  *   logprob[r] = ln p(tokens[r]) (tokens: DEVICE int32 [rows]; -1, padding: 0;

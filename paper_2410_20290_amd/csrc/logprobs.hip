@@ -299,7 +299,10 @@ logprob_kernel(LogprobArgs a, int chunks, int chunk_len, float k, float inv_t) {
 }
 
 // A wave joins a row's chunks, lane c holding chunk c: the sums by a butterfly
-// and the alternatives by taking the best of the chunks' next words each time.
+// and the alternatives by taking the best of the chunks' next words each time
+// (ranking the words that can be among them took 13.4 us a call instead of 14.9
+// on 128256 entries with top 20, but 9.0 instead of 8.1 with top 1 and 16.6
+// instead of 14.5 on 32000 with top 20).
 template <typename T>
 __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a, int chunks, float k, float inv_t) {
   __shared__ uint64_t words[kLpMaxChunks * kLpTop];
@@ -342,7 +345,9 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a, int chu
 }
 
 // Chunks of a row: of whole rounds of the waves' tiles, enough for about
-// kLpTarget work-groups.
+// kLpTarget work-groups (512 rows of 128256 with 5 alternatives 65.5 us with
+// twice as many, 61.5 with these, with 32 alternatives 96 and 82: every chunk
+// finds its alternatives anew).
 constexpr int kLpTarget = 1024;
 static int logprob_chunk_len(int rows, int vocab) {
   const int round = kLpWaves * kLpTile;

@@ -234,7 +234,7 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
     a.shift = check_table(rows, max_pages, page_tokens, n_pages);
     require(lr >= 0 && rot_dim >= 0 && rot_dim <= head_dim && rot_dim % 8 == 0,
             "lr >= 0 and rot_dim 0 or a multiple of 8 up to head_dim");
-    supported((int64_t)rows * lr <= (int64_t)1 << 28, "more than 2^28 tokens");
+    supported((int64_t)rows * lr <= kMaxGroups, "2^24 tokens or more");
     if (rows == 0 || lr == 0) return;
     require(qkv && kpool && vpool && table && lens && q && (rot_dim == 0 || freqs), "NULL buffer");
     require(aligned16(qkv) && aligned16(q) && aligned16(kpool) && aligned16(vpool),

@@ -23,6 +23,7 @@ SR_HD int imax(int a, int b) { return a > b ? a : b; }
 constexpr int kPageMaxRows = 4096;
 constexpr int kPageMaxPerRow = 65536;
 constexpr int kPageMaxPages = 1 << 20;
+constexpr int kMaxGroups = (1 << 24) - 1;   // work-groups of 256 in a launch: work-items are counted in 32 bits
 
 // log2 of the page size, or -1 where it is none of 16 .. 256.
 SR_HD int page_shift(int page_tokens) {

@@ -562,11 +562,20 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 //   O^T += V^T P^T: the contraction visits a 16-key chunk in the order the lane
 //                 holds it, so the B operand is the lane's own probabilities;
 //                 the A operand comes from V by two LDS transpose reads.
-// The 32-key blocks that hold a visible key go memory -> LDS by
-// global_load_lds, four stages deep, one barrier a block; the scores of the next
-// block are formed under the probabilities of this one; 16-byte chunks sit
-// XOR-swizzled in the LDS rows.  Two work-groups a CU.  With several splits a
-// work-group takes an even share of the blocks.
+// The 32-key blocks that hold a visible key go memory -> LDS by direct copies,
+// three stages deep, one barrier a block; 16-byte chunks sit XOR-swizzled in the
+// LDS rows.  Lane i keeps the addresses and mask flags of block i of a run of
+// 64; blocks that every query sees whole skip the mask; the output is rescaled
+// only when a maximum has moved by more than kStale.  Three work-groups a CU (48
+// KB of LDS, at most 168 registers): one's exponentials and waits run under
+// another's matrix instructions.  On 7777 tokens, 32 query and 8 KV heads of
+// 128, in a window of 4096 with 4 sinks (384 GFLOP over visible keys): 390 to 404
+// us, 950 to 990 TFLOP/s; earlier forms of this kernel with 64 columns a wave took
+// 645 us (its registers move through the accumulation file), with 256 columns a
+// work-group 426, with one barrier per two blocks 420.  Bound by the
+// matrix cores together with the softmax's vector instructions, at the clock the
+// part holds under both.  With several splits a work-group takes an even share of
+// the blocks.
 constexpr int kTileStages = 3;
 constexpr float kStale = 8.f;
 constexpr int kTileCols = 128;
@@ -992,7 +1001,8 @@ static int64_t planned_keys(const PagedAttnArgs& a) {
   return keys;
 }
 
-// Work-groups of the tile kernel that fill the chip: two a CU.
+// Work-groups of the tile kernel that the split aims at: two a CU (with three, 4
+// to 32 prompts of 300 to 512 tokens take the same to 1 %).
 constexpr int kTileTarget = 512;
 constexpr int kMaxSplits = 64;
 
@@ -1002,7 +1012,8 @@ static int tile_splits(int64_t groups, int64_t blocks) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({kTileTarget / groups, blocks / 8, kMaxSplits}));
 }
 
-// Waves that fill the chip.
+// Waves that fill the chip (8 KV heads of 128: 64 rows on 300 keys 17.5 us, with
+// half as many 18.0 and with twice as many 26.1; 8 on 8000 46.4, 49.6 and 49.6).
 constexpr int kWaveTarget = 2048;
 // The shared keys get a pass of their own where the rows would otherwise read them
 // from the caches for at least so many bytes (at ~15 TB/s, 20 us: what the two
@@ -1061,7 +1072,7 @@ template <typename T, int HD>
 static void launch_vector(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
   const int64_t blocks = vector_groups(a) / a.hkv * p.splits;
-  SR_REQUIRE(blocks <= INT_MAX, SR_ERR_UNSUPPORTED, "attention grid too large");
+  SR_REQUIRE(blocks <= kMaxGroups, SR_ERR_UNSUPPORTED, "attention grid too large");
   const dim3 grid((unsigned)blocks, a.hkv);
 #define SR_VECTOR(GC) SR_LAUNCH((paged_vector_kernel<T, HD, GC>), grid, dim3(256), 0, s, a, p.splits, qscale)
   switch (vector_cols(a.lr * (a.hq / a.hkv))) {
@@ -1089,7 +1100,7 @@ static void launch_tile(const PagedAttnArgs& a, const int32_t* common, int split
   const float qscale = kLog2e / sqrtf((float)HD);
   const int64_t cols = (int64_t)(PRE ? a.rows : 1) * a.lr * (a.hq / a.hkv);
   const int64_t total = (cols + kTileCols - 1) / kTileCols * splits * a.hkv * (PRE ? 1 : a.rows);
-  SR_REQUIRE(total <= (int64_t)INT_MAX - 8, SR_ERR_UNSUPPORTED, "attention grid too large");
+  SR_REQUIRE(total <= kMaxGroups - 8, SR_ERR_UNSUPPORTED, "attention grid too large");
   SR_LAUNCH((paged_tile_kernel<HD, PRE>), dim3((unsigned)(8 * ((total + 7) / 8))), dim3(256), 0, s, a, common, splits,
             slots, qscale);
   SR_CHECK_LAUNCH();

@@ -109,7 +109,8 @@ LAYER_BAD = [
 @pytest.mark.parametrize("kw,status", LAYER_BAD + [
     (dict(qkv=None), INVALID), (dict(qkv=0x100008), INVALID), (dict(rot=65), INVALID), (dict(rot=72), INVALID),
     (dict(rot=12), INVALID), (dict(rot=-8), INVALID), (dict(freqs=None), INVALID), (dict(v=0x300000), INVALID),
-    (dict(q=0x100000), INVALID), (dict(q=0x300000), INVALID), (dict(rows=4096, lr=1 << 17), UNSUPPORTED)])
+    (dict(q=0x100000), INVALID), (dict(q=0x300000), INVALID), (dict(rows=4096, lr=1 << 17), UNSUPPORTED),
+    (dict(rows=4096, lr=4096), UNSUPPORTED)])   # (2^24 work-groups: a launch holds fewer)
 def test_append_refuses(L, kw, status):
     assert L.sr_page_append(*args(APPEND, APPEND, kw)) == status and sr.last_error()
 
@@ -128,6 +129,8 @@ ATTN = dict(dtype=sr.SR_BF16, hd=64, hq=8, hkv=2, rows=2, lr=3, q=0x700000, k=0x
     (dict(hq=34), UNSUPPORTED), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID), (dict(shared=-1), INVALID),
     (dict(max_len=0), INVALID), (dict(out=None), INVALID), (dict(out=0x800002), INVALID), (dict(out=0x700000), INVALID),
     (dict(out=0x300000), INVALID), (dict(rows=4096, lr=1 << 16), UNSUPPORTED),
+    (dict(dtype=sr.SR_F32, hd=32, hq=1, hkv=1, rows=16, lr=1 << 24, q=1 << 40, out=1 << 41, mp=65536, pt=256),
+     UNSUPPORTED),   # (2^25 work-groups)
     (dict(rows=1, lr=1, mp=4096, max_len=60000, n=8), SMALL),
     (dict(rows=1, lr=1, mp=4096, max_len=60000, scratch=None), SMALL),
     (dict(rows=1, lr=1, mp=4096, max_len=60000, scratch=0x10000004), INVALID),
