@@ -683,17 +683,6 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   const int i0 = (int)((int64_t)kb.count * split / splits), i1 = (int)((int64_t)kb.count * (split + 1) / splits);
   const int ntile = i1 - i0;
 
-  // The wave's 32 queries, 16 bytes per lane along whole rows (clamped rows;
-  // results of columns that are no query are dropped)
-  constexpr int LPR = HD / 4, RPQ = 64 / LPR, NQ = 32 / RPQ;   // lanes per query, queries per load, loads
-  float4 qv[NQ];
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int x = imin(xw + RPQ * i + lane / LPR, X - 1), tok = x / g;
-    qv[i] = reinterpret_cast<const float4*>(
-        a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
-  }
-
   // Where blocks [64 c, 64 c + 64) of this split lie: lane i holds, for block 64
   // c + i, the addresses of its halves' keys and values (of zeros where no page
   // holds them) and its flags, so that issuing a block's copies costs a few lane
@@ -707,6 +696,13 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
   uint32_t flags = 0;
   uint2 at[2][2];           // [keys, values][half]
+  int entry[2];             // what the table says of block first + lane's halves
+  auto read_table = [&](int first) {
+    const int k0 = kb.key0(i0 + first + lane);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      entry[u] = first + lane < ntile && kb.any16(k0 + 16 * u) ? tab[(k0 + 16 * u) >> a.shift] : -1;
+  };
   auto look_up = [&](int first) {
     const int k0 = kb.key0(i0 + first + lane);
     flags = kb.all32(k0) ? 0 : PARTLY;
@@ -715,8 +711,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int k = k0 + 16 * u;
-      int page = first + lane < ntile && kb.any16(k) ? tab[k >> a.shift] : -1;
-      if ((uint32_t)page >= (uint32_t)a.n_pages) page = -1;
+      const int page = (uint32_t)entry[u] < (uint32_t)a.n_pages ? entry[u] : -1;
       const int64_t off = page < 0 ? 0 : page_offset(page, a.hkv, h, a.shift, k, HD);
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
@@ -727,6 +722,22 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       if (page < 0) flags |= EDGE | (u ? GONE1 : GONE0);
     }
   };
+  // The table first, so that the first keys do not wait behind the queries.
+  read_table(0);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // The wave's 32 queries, 16 bytes per lane along whole rows (clamped rows;
+  // results of columns that are no query are dropped)
+  constexpr int LPR = HD / 4, RPQ = 64 / LPR, NQ = 32 / RPQ;   // lanes per query, queries per load, loads
+  float4 qv[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int x = imin(xw + RPQ * i + lane / LPR, X - 1), tok = x / g;
+    qv[i] = reinterpret_cast<const float4*>(
+        a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
   // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
   // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
   // stored there, from a buffer resource at its 16-key half (no vector
@@ -742,7 +753,10 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   }
   uint32_t ring = 0;   // four flags for each stage
   auto issue = [&](int tile, int buf) {
-    if ((tile & 63) == 0) look_up(tile);
+    if ((tile & 63) == 0) {
+      if (tile > 0) read_table(tile);
+      look_up(tile);
+    }
     const int from = tile & 63;
     bf16_t* kd = lds + buf * 2 * TILE;
     const uint32_t f = __builtin_amdgcn_readlane(flags, from);
