@@ -981,16 +981,17 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
   const float L = wave_sum(x.y * wx + y.y * wy);
   constexpr int N = HD < 64 ? 1 : HD / 64;   // dimensions of a lane
   float A[N] = {};
-  if (N * lane < HD) {
-    const float* o = pt.o(th, 0, HD) + N * lane;
-    for (int s = 0; s < slots; ++s) {
-      const float w = __shfl(s < 64 ? wx : wy, s & 63, 64);
+  // (every lane stays on, those without dimensions too: they hold weights)
+  const bool mine = N * lane < HD;
+  const float* o = pt.o(th, 0, HD) + (mine ? N * lane : 0);
+  for (int s = 0; s < slots; ++s) {
+    const float w = __shfl(s < 64 ? wx : wy, s & 63, 64);
 #pragma unroll
-      for (int e = 0; e < N; ++e) A[e] += w * o[(int64_t)s * HD + e];
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) ((T*)a.out)[th * HD + N * lane + e] = from_f32<T>(L > 0.f ? A[e] / L : 0.f);
+    for (int e = 0; e < N; ++e) A[e] += w * o[(int64_t)s * HD + e];
   }
+  if (!mine) return;
+#pragma unroll
+  for (int e = 0; e < N; ++e) ((T*)a.out)[th * HD + N * lane + e] = from_f32<T>(L > 0.f ? A[e] / L : 0.f);
 }
 
 // ------------------------------------------------------------------ plan

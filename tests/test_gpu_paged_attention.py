@@ -170,6 +170,13 @@ def test_long_rows_split_over_work_groups(bf16, hd, hq, hkv):
     case(27, bf16, hd, hq, hkv, [2100, 333], 33, 64, n_new=[33, 20], max_len=4000)
 
 
+@pytest.mark.parametrize("bf16,hd,hq,hkv", [(False, 32, 1, 1), (True, 32, 2, 1), (False, 64, 1, 1), (False, 128, 2, 1),
+                                            (True, 64, 1, 1), (True, 128, 4, 1)])
+def test_rows_in_more_than_32_splits(bf16, hd, hq, hkv):
+    case(53, bf16, hd, hq, hkv, [17001], 1, 64)
+    case(54, bf16, hd, hq, hkv, [17400, 9000], 1, 128, n_new=[1, 0])
+
+
 def test_lengths_past_the_table_are_clamped():
     torch, sr = need_gpu()
     rng = np.random.default_rng(28)
