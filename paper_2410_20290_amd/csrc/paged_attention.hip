@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // KB of LDS, at most 168 registers): one's exponentials and waits run under
 // another's matrix instructions.  On 7777 tokens, 32 query and 8 KV heads of
 // 128, in a window of 4096 with 4 sinks (384 GFLOP over visible keys): 390 to 404
-// us, 950 to 990 TFLOP/s; earlier forms of this kernel with 64 columns a wave took
+// us, 950 to 990 TFLOP/s (454 in an uninterrupted run); earlier forms of this kernel with 64 columns a wave took
 // 645 us (its registers move through the accumulation file), with 256 columns a
 // work-group 426, with one barrier per two blocks 420.  Bound by the
 // matrix cores together with the softmax's vector instructions, at the clock the
