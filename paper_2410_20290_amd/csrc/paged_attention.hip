@@ -1038,7 +1038,8 @@ static int64_t planned_keys(const PagedAttnArgs& a) {
 }
 
 // Work-groups of the tile kernel that the split aims at: two a CU (with three, 4
-// to 32 prompts of 300 to 512 tokens take the same to 1 %).
+// to 32 prompts of 300 to 512 tokens take the same to 1 %; 512 rows on 2048 shared
+// keys 149 us, with three 155, with one 160).
 constexpr int kTileTarget = 512;
 constexpr int kMaxSplits = 64;
 
