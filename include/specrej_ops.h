@@ -143,8 +143,10 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
  *   j <= p and (window == 0 or j > p - window or j < sinks);
  * out[r][t][i head_dim + d] (DEVICE dtype [rows][lr][n_heads head_dim]) =
  * sum_j softmax_j(q_i . key_j / sqrt(head_dim)) value_j[d], KV head
- * floor(i n_kv_heads / n_heads); 0 where nothing is visible.  n_new as in
- * sr_page_append; rows of out past n_new[r] are not written.
+ * floor(i n_kv_heads / n_heads); 0 where nothing is visible, or every score is
+ * -inf.  n_new as in sr_page_append; rows of out past n_new[r] are not written.
+ * A NaN in a query, or in a key or value that it sees, gives NaN in the outputs
+ * that depend on it and in no others.
  * Slots that no query of a row sees (past its length, behind its window, in
  * entries that name no page) may hold anything, NaN included; a key or value
  * that one query sees and another query of the call does not must be finite.

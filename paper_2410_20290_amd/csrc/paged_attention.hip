@@ -13,7 +13,9 @@
 // Online softmax in base 2 (queries carry log2 e / sqrt(head_dim)).  A pass
 // leaves, for every token and query head, the unnormalised output, the running
 // maximum and the sum in one of the `slots` partial slots, or the output itself
-// where there is one slot.
+// where there is one slot.  A score that is NaN never raises a maximum and always
+// enters the sum, so "nothing seen" is a sum equal to 0, not one that fails to be
+// above it, and a maximum of -inf says nothing about the sum.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -195,17 +197,17 @@ __global__ void __launch_bounds__(256, 2) paged_vector_kernel(PagedAttnArgs a, i
     float M = -INFINITY;
 #pragma unroll 8
     for (int k = 0; k < NG; ++k) M = fmaxf(M, sm[k][c][HD]);
+    const float ref = M == -INFINITY ? 0.f : M;
     float L = 0.f, A = 0.f;
-    if (M != -INFINITY)
 #pragma unroll 8
-      for (int k = 0; k < NG; ++k) {
-        const float w = __builtin_amdgcn_exp2f(sm[k][c][HD] - M);
-        L += sm[k][c][HD + 1] * w;
-        A += sm[k][c][dd] * w;
-      }
+    for (int k = 0; k < NG; ++k) {
+      const float w = __builtin_amdgcn_exp2f(sm[k][c][HD] - ref);
+      L += sm[k][c][HD + 1] * w;
+      A += sm[k][c][dd] * w;
+    }
     const int64_t th = ((int64_t)row * a.lr + x / g) * a.hq + h * g + x % g;
     if (splits == 1) {
-      ((T*)a.out)[th * HD + dd] = from_f32<T>(L > 0.f ? A / L : 0.f);
+      ((T*)a.out)[th * HD + dd] = from_f32<T>(L == 0.f ? 0.f : A / L);
     } else {
       pt.o(th, split, HD)[dd] = A;
       if (dd == 0) {
@@ -480,7 +482,7 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     const int64_t th = ((int64_t)row * a.lr + c / g) * a.hq + h * g + c % g;
     float M = -INFINITY, L = 0.f, A[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto add = [&](float m1, float l1, const float* o8) {
-      if (m1 == -INFINITY) return;
+      if (l1 == 0.f) return;   // nothing seen
       const float mn = fmaxf(M, m1), ca = __builtin_amdgcn_exp2f(M - mn), cb = __builtin_amdgcn_exp2f(m1 - mn);
       M = mn;
       L = L * ca + l1 * cb;
@@ -514,7 +516,7 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       add(ws[HD], ws[HD + 1], o8);
     }
     if (splits == 1) {
-      const float inv = L > 0.f ? 1.f / L : 0.f;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
       bf16x8 r;
 #pragma unroll
       for (int e = 0; e < 8; ++e) r[e] = (__bf16)(A[e] * inv);
@@ -949,7 +951,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     }
     return;
   }
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
   wait_barrier(std::integral_constant<int, 0>{});   // every wave is done with the blocks
   // The outputs pass through the wave's slice of LDS (chunks placed like K's),
   // so that a query's leave as one contiguous run.
@@ -1012,7 +1014,7 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a, int s
   }
   if (!mine) return;
 #pragma unroll
-  for (int e = 0; e < N; ++e) ((T*)a.out)[th * HD + N * lane + e] = from_f32<T>(L > 0.f ? A[e] / L : 0.f);
+  for (int e = 0; e < N; ++e) ((T*)a.out)[th * HD + N * lane + e] = from_f32<T>(L == 0.f ? 0.f : A[e] / L);
 }
 
 // ------------------------------------------------------------------ plan
