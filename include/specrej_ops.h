@@ -147,6 +147,8 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
  * -inf.  n_new as in sr_page_append; rows of out past n_new[r] are not written.
  * A NaN in a query, or in a key or value that it sees, gives NaN in the outputs
  * that depend on it and in no others.
+ * An infinite value gives infinite outputs (NaN where signs meet, or where its
+ * weight is 0 in fp32); an infinite query or key may give NaN.
  * Slots that no query of a row sees (past its length, behind its window, in
  * entries that name no page) may hold anything, NaN included; a key or value
  * that one query sees and another query of the call does not must be finite.

@@ -60,6 +60,7 @@ struct KeyBlocks {
     if (end <= from) count = imin(count, nsink);
   }
   SR_HD int key0(int i) const { return 32 * (first + i + (i >= nsink ? gap : 0)); }
+  SR_HD bool has(int k) const { return k < end && (k < sinks || k >= lo); }
   // Whether the 16 keys from a on hold one of them.
   SR_HD bool any16(int a) const { return a < end && (a < sinks || a + 16 > lo); }
   // Whether all 32 keys from a on are among them.

@@ -240,8 +240,9 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 // The next block's keys and values are in flight while one is computed.  A
 // block's 16-key halves lie in one page each; lane i holds the page numbers of
 // block i of a run of 64, so a block's addresses cost two lane reads.  The keys
-// below common[row] are another pass's.  Lanes
-// whose key nobody sees read a visible key of the half instead (KeyBlocks::safe).
+// below common[row] are another pass's.  Lanes whose key nobody sees read a visible
+// key of the half instead (KeyBlocks::safe), and past the end of the half for its
+// value, which gives zeros (0 times the infinity of a neighbour would be NaN).
 // Bound by memory: each key and value byte is read once (8 KV heads of 128: 3 rows
 // of 20011 to 40007 keys 369 MB in 79 us, 4.7 TB/s; 512 tails of 63 to 380 keys 464
 // MB in 105 us, 4.4 TB/s; 64 rows in a window of 1024, 8 heads of 64, 135 MB in 25
@@ -309,13 +310,14 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       for (int st = 0; st < KS; ++st)
         kr[u][st] = *reinterpret_cast<const uint4*>(src + (j[u] * HD + 8 * fg + 32 * st));
     }
-    const BufRsrc rv[2] = {buf_rsrc(at(a.vpool, pg[0], k0)), buf_rsrc(at(a.vpool, pg[1], k0 + 16))};
+    constexpr int HALF = 16 * HD * 2;   // bytes
+    const BufRsrc rv[2] = {buf_rsrc(at(a.vpool, pg[0], k0), HALF), buf_rsrc(at(a.vpool, pg[1], k0 + 16), HALF)};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int u = i * KPD / 16, kk = i * KPD + lane / CPK;   // half, key of the block
-      int jj = kk - 16 * u;
-      if (!whole && pg[u] >= 0) jj = kb.safe(k0 + 16 * u, k0 + kk) - (k0 + 16 * u);
-      dma16(rv[u], (uint32_t)((jj * HD + 8 * vslot<CPK>(kk, lane % CPK)) * 2), 0, vbuf + buf * VB + i * 512);
+      uint32_t off = (uint32_t)(((kk - 16 * u) * HD + 8 * vslot<CPK>(kk, lane % CPK)) * 2);
+      if (!whole && !kb.has(k0 + kk)) off = HALF;
+      dma16(rv[u], off, 0, vbuf + buf * VB + i * 512);
     }
   };
 
@@ -599,6 +601,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   constexpr int TILE = KT * HD;                // bf16 elements of a K (or V) block
   constexpr int RPI = 64 / CPK;                // keys per copy instruction (1 KB)
   constexpr int DPW = KT / RPI / NW;           // copies per wave of a K (or V) block
+  constexpr int HALF = 16 * HD * 2;            // bytes of 16 keys
   constexpr int CPW = 2 * DPW;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[kTileStages * 2 * TILE];
   __shared__ int bounds[NW][2];
@@ -752,8 +755,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   // Copies: instruction i of a wave moves keys RPI (wave + NW i) .. of the
   // block; lane l writes slot l % CPK of key l / CPK and fetches the chunk
   // stored there, from a buffer resource at its 16-key half (no vector
-  // arithmetic where every key is seen).  A key nobody sees is replaced by one
-  // of its half that somebody does, a half without any by zeros.
+  // arithmetic where every key is seen).  Keys and values that nobody sees are read
+  // past the end of the half, as zeros, or from zeros where no page holds them.
   auto vswz = [](int k) { return HD == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2; };
   uint32_t kcopy[DPW], vcopy[DPW];   // byte offsets in the half
 #pragma unroll
@@ -774,7 +777,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     ring = (ring & ~(15u << (4 * buf))) | (f & 15u) << (4 * buf);
     auto source = [&](const uint2& v) {
       const uint32_t lo = __builtin_amdgcn_readlane(v.x, from), hi = __builtin_amdgcn_readlane(v.y, from);
-      return buf_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo));
+      return buf_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo), HALF);
     };
     uint32_t ko[DPW], vo[DPW];
 #pragma unroll
@@ -785,11 +788,8 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     if (f & PARTLY) {
 #pragma unroll
       for (int i = 0; i < DPW; ++i) {
-        const int r0 = RPI * (wave + NW * i);
-        if (f & (r0 >> 4 ? GONE1 : GONE0)) continue;
-        const int k = kb.key0(i0 + tile) + r0 + lane / CPK, d = kb.safe(k & ~15, k) - k;
-        ko[i] += (uint32_t)(d * HD * 2);
-        vo[i] += (uint32_t)(d * HD * 2);
+        if (kb.has(kb.key0(i0 + tile) + RPI * (wave + NW * i) + lane / CPK)) continue;
+        ko[i] = vo[i] = HALF;
       }
     }
 #pragma unroll

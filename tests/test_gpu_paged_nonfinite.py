@@ -127,3 +127,32 @@ def test_a_key_or_value_that_is_no_number(name, value):
             if r == hurt or key < m.shared:
                 none[r, :, h * m.g:(h + 1) * m.g, d if value else slice(None)] = True
         m.check(out, rows, none)
+
+
+@pytest.mark.parametrize("name", list(CASES))
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_an_infinite_value(name, sign):
+    """An infinity in a value that every query of the call sees, beside slots that
+    none sees: that dimension of the outputs is infinite, all else is as it was
+    (a slot that nobody sees takes no part, whatever is read in its place)."""
+    torch, sr = need_gpu()
+    say(f"infinite value {name}")
+    m = Made(name)
+    hurt = len(m.new) // 2 if len(m.new) > 2 else 0
+    keys = visible_to_all(m, hurt)
+    if m.lr == 1:
+        keys.append(int(m.cache.lens[hurt]) - 1)            # the last: free slots beside it
+    for i, key in enumerate(keys):
+        pg, slot = m.at(hurt, key)
+        h, d = i % m.hkv, (13 * i + 5) % m.hd
+        kept = m.cache.v[pg, h, slot, d]
+        m.cache.v[pg, h, slot, d] = sign * np.inf
+        out = m.gpu(torch, sr)
+        m.cache.v[pg, h, slot, d] = kept
+        rows = sorted({hurt} | set(some(m)))
+        hit = np.zeros(m.q.shape, dtype=bool)
+        for r in rows:
+            if r == hurt or key < m.shared:
+                hit[r, :m.new[r], h * m.g:(h + 1) * m.g, d] = True
+        assert (out[hit] == sign * np.inf).all(), (key, out[hit])
+        m.check(np.where(hit, np.nan, out), rows, hit)
