@@ -63,7 +63,10 @@ sr_status sr_page_fork(const int32_t *table, const int32_t *lens, int32_t rows, 
  *    copied.  One row may keep the page: if every entry that names it is the
  *    part-filled last page of a row adding tokens, the lowest such row does.
  *    A part-filled last page whose entry names no page is replaced by a new
- *    page, without a copy.
+ *    page, without a copy: the row's len % page_tokens tokens in it, masked
+ *    until then, would be whatever the page held before.  The caller writes
+ *    them again, with the new ones (sr_page_append with n_new = len %
+ *    page_tokens + the added tokens), before a call reads the row.
  *  - All or nothing: info (DEVICE int32 [4]) receives the missing pages, the
  *    rows whose new length passes max_pages * page_tokens, and, if both are
  *    0, the pages taken and the pages copied.  Otherwise nothing is reserved

@@ -495,7 +495,9 @@ def page_fork(table, lens, parent, page_tokens: int, table_out, lens_out, refs_o
 
 def page_reserve(pool, table, lens, refs, n_add, table_out, lens_out, refs_out, granted, info, stream=None):
     """sr_page_reserve: room for n_add tokens (int32 [rows], or one number for
-    every row).  table_out, lens_out and refs_out may be the inputs."""
+    every row).  table_out, lens_out and refs_out may be the inputs.  A row
+    whose part-filled last page is lost gets a new one, whose earlier tokens the
+    caller writes again."""
     import torch
     i32 = torch.int32
     pa, n_pages = _pool_args(pool)
