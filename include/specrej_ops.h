@@ -70,10 +70,10 @@ sr_status sr_page_fork(const int32_t *table, const int32_t *lens, int32_t rows, 
  *  - All or nothing: info (DEVICE int32 [4]) receives the missing pages, the
  *    rows whose new length passes max_pages * page_tokens, and, if both are
  *    0, the pages taken and the pages copied.  Otherwise nothing is reserved
- *    (those two are 0) and the outputs equal the inputs.
- * granted[r] = tokens reserved (0 in that case), lens_out = lens + granted,
- * table_out, refs_out: the new table (-1 past the new lengths and for entries
- * that name no page) and counts.  table_out, lens_out and refs_out may each be
+ *    (those two are 0) and the outputs are the rows and counts as they were.
+ * granted[r] = tokens reserved (0 in that case), lens_out = lens (clamped) +
+ * granted, table_out, refs_out: the new table (-1 past lens_out and for entries
+ * that name no page, in either case) and counts.  table_out, lens_out and refs_out may each be
  * the input itself; any other overlap is an error.  pool: DEVICE, elements of
  * elem_bytes 2 or 4.  scratch: DEVICE int32 of scratch_elems >=
  * sr_page_reserve_scratch(rows, max_pages, n_pages) elements. */
