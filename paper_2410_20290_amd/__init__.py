@@ -433,6 +433,13 @@ def _sizes(t, name: str, dtypes, dims: int):
     return t.shape
 
 
+def _int32(*values):
+    """Refuses numbers that a C int cannot hold (ctypes would pass their lower half)."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise ValueError(f"{v} does not fit 32 bits")
+
+
 def _run(tensors, stream, call, args, need=0, scratch_type=None, at=None):
     """call(*args, stream) on the tensors' device; with `need` elements of
     scratch, allocated on that stream, their address and number go in at
@@ -488,6 +495,7 @@ def page_fork(table, lens, parent, page_tokens: int, table_out, lens_out, refs_o
     _expect(lens, "lens", i32, (rows,))
     _expect(table_out, "table_out", i32, (n, mp))
     _expect(lens_out, "lens_out", i32, (n,))
+    _int32(rows, n, n_pages, page_tokens, window, sinks)
     _run((refs_out, table, lens, parent, table_out, lens_out), stream, lib().sr_page_fork,
          (table.data_ptr(), lens.data_ptr(), rows, mp, parent.data_ptr(), n, page_tokens, n_pages, window, sinks,
           table_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr()))
@@ -509,9 +517,13 @@ def page_reserve(pool, table, lens, refs, n_add, table_out, lens_out, refs_out, 
     each = n_add if torch.is_tensor(n_add) else None
     if each is not None:
         _expect(each, "n_add", i32, (rows,))
+    same = 0 if each is not None else int(n_add)
+    if each is None and same != n_add:
+        raise ValueError(f"n_add: expected a whole number, got {n_add}")
+    _int32(same)
     L = lib()
     _run((pool, table, lens, refs, each, table_out, lens_out, refs_out, granted, info), stream, L.sr_page_reserve,
-         (*pa, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), rows, mp, _ptr(each), 0 if each is not None else int(n_add),
+         (*pa, table.data_ptr(), lens.data_ptr(), refs.data_ptr(), rows, mp, _ptr(each), same,
           table_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(), granted.data_ptr(), info.data_ptr()),
          L.sr_page_reserve_scratch(rows, mp, n_pages), i32, 20)
 
@@ -535,6 +547,7 @@ def page_compact(pool, table, lens, refs, table_out, refs_out, info, stream=None
 def rope_frequencies(rot_dim: int, theta: float, scaling: int = SR_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
                      high: float = 4.0, n: float = 8192.0) -> np.ndarray:
     """sr_rope_frequencies: float64 [rot_dim / 2], radians a position."""
+    _int32(rot_dim, scaling)
     out = np.zeros(max(1, rot_dim // 2))
     _check(lib().sr_rope_frequencies(rot_dim, theta, scaling, factor, low, high, n, out.ctypes.data))
     return out
@@ -583,6 +596,7 @@ def paged_attention(q, kpool, vpool, table, lens, out, n_new=None, window: int =
     _expect(out, "out", out.dtype, (rows, lr, hq * hd))
     if max_len is None:
         max_len = max(1, mp * pt)
+    _int32(window, sinks, shared, max_len)
     L = lib()
     _run((q, kpool, vpool, table, lens, out, n_new), stream, L.sr_paged_attention,
          (dtype, hd, hq, hkv, rows, lr, q.data_ptr(), kpool.data_ptr(), vpool.data_ptr(), pt, n_pages, table.data_ptr(), mp,
@@ -609,6 +623,7 @@ def token_logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logp
                                 (top_logprobs, "top_logprobs", torch.float32, (rows, top))):
         if t is not None:
             _expect(t, name, typ, shape)
+    _int32(rows, vocab)
     L = lib()
     _run((logits, tokens, logprob, entropy, top_ids, top_logprobs), stream, L.sr_token_logprobs,
          (SR_F32 if logits.dtype is torch.float32 else SR_BF16, logits.data_ptr(), stride, rows, vocab, temperature,
