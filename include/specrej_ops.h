@@ -164,8 +164,9 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
  * max_len: the longest row the caller expects (plans the split of the work over
  * the keys; rows may be longer), >= 1.
  * head_dim in {32, 64, 128}; n_heads / n_kv_heads <= 16; rows * lr * n_heads <=
- * 2^28; calls of 2^24 work-groups (of 1 to 8 query columns, prompts in bf16 of
- * 128) are refused.  bf16 with head_dim 64 or 128 runs on the matrix cores:
+ * 2^28; calls of 2^24 work-groups are refused, counted for one KV head where
+ * they hold up to 8 query columns (fp32, head_dim 32) and for all of them where
+ * they hold 128 (prompts in bf16).  bf16 with head_dim 64 or 128 runs on the matrix cores:
  * probabilities rounded to bf16, sums in fp32, queries in 16 bits where a row
  * has at most 8 query columns, rounded to bf16 elsewhere and for the shared
  * part.  q, kpool, vpool, out 16-byte aligned.  scratch: DEVICE float of

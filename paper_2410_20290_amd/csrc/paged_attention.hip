@@ -6,8 +6,9 @@
 //   paged_tile_kernel    (bf16): 128 query columns a work-group, keys staged in
 //                        LDS for all of them: prompts, and the part of the rows
 //                        that lies in the pages of row 0, once for all rows
-//   paged_vector_kernel  (fp32, head_dim 32): one token and a few query heads
-//                        of a KV head per work-group, vector ALU
+//   paged_vector_kernel  (fp32, and bf16 with head_dim 32): up to eight query
+//                        columns of a row and KV head per work-group, of one token
+//                        or several, vector ALU
 //   paged_merge_kernel   joins the partials of a token's work-groups
 //
 // Online softmax in base 2 (queries carry log2 e / sqrt(head_dim)).  A pass
@@ -1129,15 +1130,6 @@ static void launch_vector(const PagedAttnArgs& a, const PagedPlan& p, hipStream_
   if (p.splits > 1) launch_merge<T, HD>(a, p.splits, s);
 }
 
-template <typename T>
-static void vector_by_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
-  switch (a.hd) {
-    case 32: launch_vector<T, 32>(a, p, s); break;
-    case 64: launch_vector<T, 64>(a, p, s); break;
-    default: launch_vector<T, 128>(a, p, s); break;
-  }
-}
-
 template <int HD, bool PRE>
 static void launch_tile(const PagedAttnArgs& a, const int32_t* common, int splits, int slots, hipStream_t s) {
   const float qscale = kLog2e / sqrtf((float)HD);
@@ -1192,8 +1184,15 @@ void paged_attn(const PagedAttnArgs& a, hipStream_t s) {
     else matrix_cores<64>(a, p, s);
     return;
   }
-  if (a.dtype == SR_BF16) vector_by_hd<bf16_t>(a, p, s);
-  else vector_by_hd<float>(a, p, s);
+  if (a.dtype == SR_BF16) {   // (head_dim 32: the others take the matrix cores)
+    launch_vector<bf16_t, 32>(a, p, s);
+    return;
+  }
+  switch (a.hd) {
+    case 32: launch_vector<float, 32>(a, p, s); break;
+    case 64: launch_vector<float, 64>(a, p, s); break;
+    default: launch_vector<float, 128>(a, p, s); break;
+  }
 }
 
 }  // namespace sr
