@@ -73,9 +73,9 @@ sr_status sr_page_fork(const int32_t *table, const int32_t *lens, int32_t rows, 
  *    (those two are 0) and the outputs are the rows and counts as they were.
  * granted[r] = tokens reserved (0 in that case), lens_out = lens (clamped) +
  * granted, table_out, refs_out: the new table (-1 past lens_out and for entries
- * that name no page, in either case) and counts.  table_out, lens_out and refs_out may each be
- * the input itself; any other overlap is an error.  pool: DEVICE, elements of
- * elem_bytes 2 or 4.  scratch: DEVICE int32 of scratch_elems >=
+ * that name no page, in either case) and counts.  table_out, lens_out and
+ * refs_out may each be the input itself; any other overlap is an error.  pool:
+ * DEVICE, elements of elem_bytes 2 or 4.  scratch: DEVICE int32 of scratch_elems >=
  * sr_page_reserve_scratch(rows, max_pages, n_pages) elements. */
 sr_status sr_page_reserve(void *pool, int64_t block_elems, int32_t n_layers, int32_t n_kv_heads,
                           int32_t head_dim, int32_t elem_bytes, int32_t page_tokens, int32_t n_pages,
@@ -166,11 +166,11 @@ sr_status sr_page_append(int32_t dtype, int32_t head_dim, int32_t n_heads, int32
  * head_dim in {32, 64, 128}; n_heads / n_kv_heads <= 16; rows * lr * n_heads <=
  * 2^28; calls of 2^24 work-groups are refused, counted for one KV head where
  * they hold up to 8 query columns (fp32, head_dim 32) and for all of them where
- * they hold 128 (prompts in bf16).  bf16 with head_dim 64 or 128 runs on the matrix cores:
- * probabilities rounded to bf16, sums in fp32, queries in 16 bits where a row
- * has at most 8 query columns, rounded to bf16 elsewhere and for the shared
- * part.  q, kpool, vpool, out 16-byte aligned.  scratch: DEVICE float of
- * scratch_elems >= sr_paged_attention_scratch(...) elements. */
+ * they hold 128 (prompts in bf16).  bf16 with head_dim 64 or 128 runs on the
+ * matrix cores: probabilities rounded to bf16, sums in fp32, queries in 16 bits
+ * where a row has at most 16 query columns, rounded to bf16 where it has more.
+ * q, kpool, vpool, out 16-byte aligned.  scratch: DEVICE float of scratch_elems
+ * >= sr_paged_attention_scratch(...) elements. */
 sr_status sr_paged_attention(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
                              int32_t rows, int32_t lr, const float *q, const void *kpool,
                              const void *vpool, int32_t page_tokens, int32_t n_pages,

@@ -226,11 +226,13 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 
 // bf16, head_dim 64 or 128, at most 16 query columns: column x is token x / G of
 // the row's, query head x % G of the KV head's G, so the columns' queries and
-// outputs are contiguous.  Up to eight columns are there twice: 0 .. 7 hold the
-// queries rounded to bf16 and 8 .. 15 what the rounding left, also in bf16, and
-// the two scores are added, so that the queries keep 16 bits at no product more
-// (the output is then 0.0019 to 0.0020 off in the 2-norm instead of 0.0032, of
-// which 0.0017 are its own rounding).  Work-group = (split, KV head, row), NW
+// outputs are contiguous.  The queries are rounded to bf16 and so is what that
+// leaves of them, and the two scores are added, so that they keep 16 bits (the
+// output is then 0.0019 to 0.0020 off in the 2-norm instead of 0.0028 to 0.0030, of
+// which 0.0017 are its own rounding).  TWICE: up to eight columns are there twice,
+// 0 .. 7 the first part and 8 .. 15 the second, at no product more; more columns
+// take a second product (64 rows of 300 to 900 keys, 8 KV heads of 128, 12 columns:
+// 36.8 us with it and 36.7 without).  Work-group = (split, KV head, row), NW
 // waves; every wave takes an even share of the 32-key blocks that hold visible
 // keys and waits on no other until the merge.
 //   S^T = K Q^T   (v_mfma_f32_16x16x32_bf16): the A operand, 16 keys x 32 dims,
@@ -248,7 +250,7 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 // of 20011 to 40007 keys 369 MB in 79 us, 4.7 TB/s; 512 tails of 63 to 380 keys 464
 // MB in 105 us, 4.4 TB/s; 64 rows in a window of 1024, 8 heads of 64, 135 MB in 25
 // us, 5.4 TB/s).
-template <int HD, int NW>
+template <int HD, int NW, bool TWICE>
 __global__ void __launch_bounds__(64 * NW)
 paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
   constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
@@ -262,8 +264,7 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fg = lane >> 4;
   const int g = a.hq / a.hkv;
-  const bool twice = a.lr * g <= 8;
-  const int x = twice ? fr & 7 : fr, t = x / g;    // this lane's column
+  const int x = TWICE ? fr & 7 : fr, t = x / g;    // this lane's column
   const bool live = t < rs.n;
   const int end_c = rs.p0 + (live ? t : 0) + 1, lo_c = window_start(end_c - 1, a.window);
   const int lo_last = window_start(rs.len - 1, a.window);
@@ -328,7 +329,7 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   if (i0 < i1) load_block(0, ka, 0);
 
   // Q^T fragments (B operand): lane holds Q[column fr][32 s + 8 fg .. + 8]
-  bf16x8 qf[KS];
+  bf16x8 qf[KS], ql[TWICE ? 1 : KS];
   {
     const float* qr = a.q + (((int64_t)row * a.lr + (live ? t : 0)) * a.hq + h * g + (live ? x - t * g : 0)) * HD;
 #pragma unroll
@@ -340,7 +341,9 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       for (int e = 0; e < 8; ++e) {
         const float full = v[e] * qscale;
         const __bf16 top = (__bf16)full;
-        qf[st][e] = twice && fr >= 8 ? (__bf16)(full - (float)top) : top;
+        const __bf16 left = (__bf16)(full - (float)top);
+        qf[st][e] = TWICE && fr >= 8 ? left : top;
+        if constexpr (!TWICE) ql[st][e] = left;
       }
     }
   }
@@ -364,8 +367,11 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     for (int u = 0; u < 2; ++u) {
       st[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s2 = 0; s2 < KS; ++s2)
+      for (int s2 = 0; s2 < KS; ++s2) {
         st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[u][s2]), qf[s2], st[u], 0, 0, 0);
+        if constexpr (!TWICE)
+          st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[u][s2]), ql[s2], st[u], 0, 0, 0);
+      }
     }
     const int k0 = kb.key0(base + b);
     int pg[2];
@@ -376,7 +382,7 @@ paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
       sv[i] = st[0][i];
       sv[4 + i] = st[1][i];
     }
-    if (twice) {   // the other of lanes fr and fr ^ 8 (a rotation by 8 of 16)
+    if constexpr (TWICE) {   // the other of lanes fr and fr ^ 8 (a rotation by 8 of 16)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         sv[i] += __builtin_bit_cast(
@@ -576,7 +582,8 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // LDS rows.  Lane i keeps the addresses and mask flags of block i of a run of
 // 64; blocks that every query sees whole skip the mask; the output is rescaled
 // only when a maximum has moved by more than kStale.  Three work-groups a CU (48
-// KB of LDS, at most 168 registers): one's exponentials and waits run under
+// KB of LDS, at most 168 registers; PRE: two, which is all that it starts, see
+// kTileTarget): one's exponentials and waits run under
 // another's matrix instructions.  On 7777 tokens, 32 query and 8 KV heads of
 // 128, in a window of 4096 with 4 sinks (384 GFLOP over visible keys): 390 to 404
 // us, 950 to 990 TFLOP/s (454 us in an uninterrupted run); earlier forms of this
@@ -586,16 +593,18 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // instructions, at the clock the part holds under both.  With several splits a
 // work-group takes an even share of the blocks.
 // Queries and probabilities are rounded to bf16 for the products: outputs are
-// 0.0030 to 0.0033 off in the 2-norm, of which 0.0017 are their own rounding (the
-// wave kernel's queries of 16 bits leave 0.0019 to 0.0020).  The queries' low part
-// would take 8 matrix instructions on a block's 16 at head_dim 128, and 32 more
-// registers, which three work-groups a CU do not leave.
+// 0.0030 to 0.0033 off in the 2-norm, of which 0.0017 are their own rounding.  The
+// queries' low part takes 8 matrix instructions on a block's 16 at head_dim 128,
+// and 32 more registers, which three work-groups a CU do not leave.  PRE has them
+// and adds it, as the wave kernel does for the rest of the same rows: 0.0022 to
+// 0.0023 instead of 0.0031 to 0.0033 (512 rows on 2048 shared keys, 8 KV heads of
+// 128, 151.5 us instead of 147.8; 8 heads of 64, 1024 shared, 106.7 instead of 106.8).
 constexpr int kTileStages = 3;
 constexpr float kStale = 8.f;
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE>
-__global__ void __launch_bounds__(256, 3)
+__global__ void __launch_bounds__(256, PRE ? 2 : 3)
 paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slots, float qscale) {
   constexpr int KT = 32, NW = 4;
   constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
@@ -813,7 +822,7 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 
   // LDS element offsets: the K fragment of key fr (chunk 2 s + fh), and the
   // four dims dt 32 + 16 (l / 16 % 2) + 4 (l % 4) .. of V key 4 fh + l % 16 / 4
-  bf16x8 qf[KS];
+  bf16x8 qf[KS], ql[PRE ? KS : 1];   // the queries in bf16, what that leaves of them
   // byte offset in a stage of chunk fh of K row fr (chunk 2 s + fh: this ^ 32 s)
   const uint32_t kbase = (uint32_t)(fr * HD + 8 * (fh ^ (fr & (CPK - 1)))) * 2;
   // LDS address in the first V block of dims 16 (l / 16 % 2) + 4 (l % 4) .. of key
@@ -855,8 +864,11 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
     f32x16 sc;
     zero(sc);
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(lds + ST * 2 * TILE, s), qf[s], sc, 0, 0, 0);
+    for (int s = 0; s < KS; ++s) {
+      const bf16x8 k = frag(lds + ST * 2 * TILE, s);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[s], sc, 0, 0, 0);
+      if constexpr (PRE) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, ql[s], sc, 0, 0, 0);
+    }
     if (f & EDGE) {                            // (uniform)
       asm volatile("");                        // (a branch, not selects on every block)
       // bit j: this lane's key j of the block (of the 32 from 4 fh on) is seen
@@ -906,16 +918,21 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
   bf16_t* const slice = lds + wave * 32 * HD;
   if (ntile > 0) {
     issue(0, 0);
+    // (through the wave's own slice: its LDS operations are in order)
     bf16_t* qs = slice + 2 * TILE;
+    auto stage_queries = [&](auto part, auto& out) {
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
-      const bf16x4 v = {(__bf16)(qv[i].x * qscale), (__bf16)(qv[i].y * qscale), (__bf16)(qv[i].z * qscale),
-                        (__bf16)(qv[i].w * qscale)};
-      *reinterpret_cast<bf16x4*>(qs + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
-    }
+      for (int i = 0; i < NQ; ++i) {
+        const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
+        const bf16x4 v = {part(qv[i].x), part(qv[i].y), part(qv[i].z), part(qv[i].w)};
+        *reinterpret_cast<bf16x4*>(qs + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
+      }
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = frag(qs, s);
+      for (int s = 0; s < KS; ++s) out[s] = frag(qs, s);
+    };
+    stage_queries([&](float v) { return (__bf16)(v * qscale); }, qf);
+    if constexpr (PRE)
+      stage_queries([&](float v) { return (__bf16)(v * qscale - (float)(__bf16)(v * qscale)); }, ql);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // every wave's queries read
     if (ntile > 1) issue(1, 1);
     auto one = [&](auto stage, int tile) {
@@ -1046,7 +1063,7 @@ static int64_t planned_keys(const PagedAttnArgs& a) {
 
 // Work-groups of the tile kernel that the split aims at: two a CU (with three, 4
 // to 32 prompts of 300 to 512 tokens take the same to 1 %; 512 rows on 2048 shared
-// keys 149 us, with three 155, with one 160).
+// keys 152 us, with three 167, with one 163).
 constexpr int kTileTarget = 512;
 constexpr int kMaxSplits = 64;
 
@@ -1061,9 +1078,11 @@ static int tile_splits(int64_t groups, int64_t blocks) {
 constexpr int kWaveTarget = 2048;
 // The shared keys get a pass of their own where the rows would otherwise read them
 // from the caches for at least so many bytes (at ~15 TB/s, 20 us: what the two
-// launches and the joining cost).  8 KV heads of 128: 64 rows on 1024 shared keys
-// 29.8 us without and 36.1 with (268 MB), 128 rows on 1024 49 and 36 (537 MB), 512
-// on 256 72 and 66; 8 heads of 64: 256 rows on 512 31.9 and 31.5 (268 MB).
+// launches and the joining cost).  8 KV heads of 128, tails of up to 60 keys: 64
+// rows on 1024 shared keys 28.6 us without and 29.5 with (268 MB), 96 on 1024 38.3
+// and 30.5 (403 MB), 128 on 1024 47 and 32 (537 MB), 512 on 256 58 and 51; beside
+// tails of 63 to 380 keys 300 on 256 80.0 and 85.7 (315 MB); 8 heads of 64: 256 rows
+// on 512 27.6 and 26.4 (268 MB).
 constexpr int64_t kShareBytes = 300 << 20;
 
 static PagedPlan paged_plan(const PagedAttnArgs& a) {
@@ -1152,9 +1171,14 @@ static void launch_wave(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t 
     launch_tile<HD, true>(a, common, p.pre, p.slots(), s);
   }
   const dim3 grid(p.splits, a.hkv, a.rows);
-#define SR_PAGED_WAVE(NW)                                                                                          \
-  SR_LAUNCH((paged_wave_kernel<HD, NW>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, p.pre, \
+#define SR_PAGED_WAVE2(NW, TWICE)                                                                                 \
+  SR_LAUNCH((paged_wave_kernel<HD, NW, TWICE>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, p.pre, \
             p.slots(), qscale)
+#define SR_PAGED_WAVE(NW)                                       \
+  do {                                                          \
+    if (a.lr * (a.hq / a.hkv) <= 8) SR_PAGED_WAVE2(NW, true);   \
+    else SR_PAGED_WAVE2(NW, false);                             \
+  } while (0)
   switch (p.nw) {
     case 8: SR_PAGED_WAVE(8); break;
     case 4: SR_PAGED_WAVE(4); break;
@@ -1162,6 +1186,7 @@ static void launch_wave(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t 
     default: SR_PAGED_WAVE(1); break;
   }
 #undef SR_PAGED_WAVE
+#undef SR_PAGED_WAVE2
   SR_CHECK_LAUNCH();
   if (p.splits > 1) launch_merge<bf16_t, HD>(a, p.slots(), s);
 }
