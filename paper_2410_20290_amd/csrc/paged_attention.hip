@@ -840,8 +840,10 @@ paged_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int split
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
   // from the lowest finite score: while a column has seen only -inf its
-  // probabilities are exp2(-inf) = 0, where -inf - -inf would be NaN
-  float m = -FLT_MAX, l = 0.f;
+  // probabilities are exp2(-inf) = 0, where -inf - -inf would be NaN; for columns
+  // that are no query from +inf, which no score of theirs passes, so that they
+  // never rescale the others (and what lies there changes no rounding)
+  float m = live ? -FLT_MAX : INFINITY, l = 0.f;
 
   auto zero = [](f32x16& sc) {
 #pragma unroll
