@@ -249,9 +249,10 @@ static __device__ __attribute__((aligned(16))) bf16_t zero_keys[16 * 128];
 // Bound by memory: each key and value byte is read once (8 KV heads of 128: 3 rows
 // of 20011 to 40007 keys 369 MB in 79 us, 4.7 TB/s; 512 tails of 63 to 380 keys 464
 // MB in 105 us, 4.4 TB/s; 64 rows in a window of 1024, 8 heads of 64, 135 MB in 25
-// us, 5.4 TB/s).
+// us, 5.4 TB/s).  head_dim 64 keeps four waves a SIMD (512 rows of 100 to 600 keys
+// 75.7 us; as the compiler chooses, three, 77.5).
 template <int HD, int NW, bool TWICE>
-__global__ void __launch_bounds__(64 * NW)
+__global__ void __launch_bounds__(64 * NW, HD == 64 ? 4 : 1)
 paged_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
   constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
   constexpr int KPD = 64 / CPK, NV = 32 / KPD;     // keys per V copy, copies of a block
