@@ -63,7 +63,8 @@ struct Partials {
 // read once for all its columns.  The groups are joined through LDS.
 // Bound by instructions: 4 FMAs, log2(HD / 4) DPP adds and an exponential per key
 // and column and lane (fp32 prompts of 2000 tokens 160 us with a column of its own
-// for every group, 87 with up to eight).
+// for every group, 87 with up to eight; four of them, 4 heads of 32, 233 us for 4.1
+// GFLOP, 18 TFLOP/s).
 template <typename T>
 __device__ __forceinline__ float4 load4(const T* p);
 template <>
@@ -584,15 +585,15 @@ __global__ void __launch_bounds__(256) paged_common_kernel(PagedAttnArgs a, int3
 // 64; blocks that every query sees whole skip the mask; the output is rescaled
 // only when a maximum has moved by more than kStale.  Three work-groups a CU (48
 // KB of LDS, at most 168 registers; PRE: two, which is all that it starts, see
-// kTileTarget): one's exponentials and waits run under
-// another's matrix instructions.  On 7777 tokens, 32 query and 8 KV heads of
-// 128, in a window of 4096 with 4 sinks (384 GFLOP over visible keys): 390 to 404
-// us, 950 to 990 TFLOP/s (454 us in an uninterrupted run); earlier forms of this
-// kernel with 64 columns a wave took 645 us (its registers move through the
-// accumulation file), with 256 columns a work-group 426, with one barrier per two
-// blocks 420.  Bound by the matrix cores together with the softmax's vector
-// instructions, at the clock the part holds under both.  With several splits a
-// work-group takes an even share of the blocks.
+// kTileTarget): one's exponentials and waits run under another's matrix
+// instructions.  On 7777 tokens, 32 query and 8 KV heads of 128, in a window of
+// 4096 with 4 sinks (384 GFLOP over visible keys): 390 to 413 us, 930 to 990 TFLOP/s
+// (463 us in an uninterrupted run); earlier forms of this kernel with 64 columns a
+// wave took 645 us (its registers move through the accumulation file), with 256
+// columns a work-group 426, with one barrier per two blocks 420.  There the matrix
+// cores are busy for 48 % and the vector ALU for 52 % of the time, at the 1.8 GHz
+// that the part holds under both.  With several splits a work-group takes an even
+// share of the blocks.
 // Queries and probabilities are rounded to bf16 for the products: outputs are
 // 0.0030 to 0.0033 off in the 2-norm, of which 0.0017 are their own rounding.  The
 // queries' low part takes 8 matrix instructions on a block's 16 at head_dim 128,
