@@ -75,7 +75,9 @@ sr_status sr_page_fork(const int32_t *table, const int32_t *lens, int32_t rows, 
  * granted, table_out, refs_out: the new table (-1 past lens_out and for entries
  * that name no page, in either case) and counts.  table_out, lens_out and
  * refs_out may each be the input itself; any other overlap is an error.  pool:
- * DEVICE, elements of elem_bytes 2 or 4.  scratch: DEVICE int32 of scratch_elems >=
+ * DEVICE, elements of elem_bytes 2 or 4; elem_bytes 1: pages of 4 bits
+ * (specrej_serving.h), head_dim their bytes a token (17, 34 or 68), of which a
+ * copied page takes all slots.  scratch: DEVICE int32 of scratch_elems >=
  * sr_page_reserve_scratch(rows, max_pages, n_pages) elements. */
 sr_status sr_page_reserve(void *pool, int64_t block_elems, int32_t n_layers, int32_t n_kv_heads,
                           int32_t head_dim, int32_t elem_bytes, int32_t page_tokens, int32_t n_pages,

@@ -2,7 +2,7 @@
 
 Argument marshalling only: every step of the hot path runs in the library's
 HIP kernels.  torch provides device memory and streams.  The names follow the
-C interface in include/specrej.h and include/specrej_ops.h.  Importing this module does not need a GPU;
+C interface in include/specrej.h, include/specrej_ops.h and include/specrej_serving.h.  Importing this module does not need a GPU;
 calling anything that launches work does, and fails loudly if the library is
 not built.
 """
@@ -19,7 +19,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libspecrej.so")
 
 SR_OK, SR_ERR_INVALID_ARG, SR_ERR_WORKSPACE_TOO_SMALL, SR_ERR_UNSUPPORTED, SR_ERR_DEVICE, SR_ERR_INTERNAL = range(6)
-SR_F32, SR_BF16 = 0, 1
+SR_F32, SR_BF16, SR_FP4 = 0, 1, 2
 
 _i32, _i64, _u64, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_double
 _vp = ctypes.c_void_p
@@ -131,8 +131,19 @@ def lib():
         L.sr_paged_attention_scratch.argtypes = [_i32] * 12
         L.sr_token_logprobs.argtypes = [_i32, _vp, _i64, _i32, _i32, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, sz, _vp]
         L.sr_token_logprobs_scratch.argtypes = [_i32, _i32, _i32]
+        L.sr_page_append_norm.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _f64, _vp, _vp,
+                                          _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp]
+        L.sr_page_read.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp,
+                                   _vp]
+        L.sr_paged_attention_fp4.argtypes = L.sr_paged_attention.argtypes
+        L.sr_paged_attention_fp4_scratch.argtypes = [_i32] * 12
+        L.sr_sample_filtered.argtypes = [_i32, _vp, _i64, _i32, _i32, _vp, _f32, _vp, _i32, _vp, _f32, _vp, _f32, _vp, _i64,
+                                         _vp, _vp, _vp, _vp, sz, _vp]
+        L.sr_sample_filtered_scratch.argtypes = [_i32, _i32]
+        for f in ("sr_page_append_norm", "sr_page_read", "sr_paged_attention_fp4", "sr_sample_filtered"):
+            getattr(L, f).restype = _i32
         for f in ("sr_page_reserve_scratch", "sr_page_compact_scratch", "sr_paged_attention_scratch",
-                  "sr_token_logprobs_scratch"):
+                  "sr_token_logprobs_scratch", "sr_paged_attention_fp4_scratch", "sr_sample_filtered_scratch"):
             getattr(L, f).restype = sz
         for f in ("sr_page_fork", "sr_page_reserve", "sr_page_compact", "sr_rope_frequencies", "sr_page_append",
                   "sr_paged_attention", "sr_token_logprobs"):
@@ -476,8 +487,10 @@ def _cache_types():
 
 
 def _pool_args(pool):
-    """(ctypes arguments, n_pages) of a pool [layers][2][n_pages][hkv][page_tokens][hd]."""
-    nl, two, n_pages, hkv, pt, hd = _sizes(pool, "pool", _cache_types(), 6)
+    """(ctypes arguments, n_pages) of a pool [layers][2][n_pages][hkv][page_tokens][hd]
+    (4 bits: uint8, 17 hd / 32 instead of hd)."""
+    import torch
+    nl, two, n_pages, hkv, pt, hd = _sizes(pool, "pool", (*_cache_types(), torch.uint8), 6)
     if two != 2:
         raise ValueError(f"pool has shape {tuple(pool.shape)}, expected [layers][2][n_pages][hkv][page_tokens][hd]")
     return (pool.data_ptr(), n_pages * hkv * pt * hd, nl, hkv, hd, pool.element_size(), pt, n_pages), n_pages
@@ -629,3 +642,137 @@ def token_logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logp
          (SR_F32 if logits.dtype is torch.float32 else SR_BF16, logits.data_ptr(), stride, rows, vocab, temperature,
           _ptr(tokens), top, _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs)),
          L.sr_token_logprobs_scratch(rows, vocab, top), torch.float32, 12)
+
+
+# ------------------------- a cache of 4 bits and the filtered draw
+# (include/specrej_serving.h)
+def fp4_token_bytes(head_dim: int) -> int:
+    """Bytes of one token's key (or value) of one KV head in a cache of 4 bits:
+    the last dimension of its uint8 pools."""
+    if head_dim not in (32, 64, 128):
+        raise ValueError(f"head_dim must be 32, 64 or 128, got {head_dim}")
+    return 17 * head_dim // 32
+
+
+def _any_layer_args(kpool, vpool, table, lens, n_new):
+    """(cache type, rows, max_pages, hkv, page_tokens, hd, n_pages); uint8 pools hold 4 bits."""
+    import torch
+    one = kpool if kpool is not None else vpool
+    if one is None:
+        raise ValueError("no pool")
+    if one.dtype is not torch.uint8:
+        return _layer_args(one, one if vpool is None else vpool, table, lens, n_new)
+    i32 = torch.int32
+    n_pages, hkv, pt, nbytes = _sizes(one, "pool", (torch.uint8,), 4)
+    if nbytes not in (17, 34, 68):
+        raise ValueError(f"a pool of 4 bits has 17, 34 or 68 bytes a token, got {nbytes}")
+    if vpool is not None:
+        _expect(vpool, "vpool", torch.uint8, one.shape)
+    rows, mp = _sizes(table, "table", (i32,), 2)
+    _expect(lens, "lens", i32, (rows,))
+    if n_new is not None:
+        _expect(n_new, "n_new", i32, (rows,))
+    return SR_FP4, rows, mp, hkv, pt, nbytes * 32 // 17, n_pages
+
+
+def page_append_norm(qkv, freqs, table, lens, kpool, vpool, q, q_norm=None, k_norm=None, eps: float = 1e-5, n_new=None,
+                     interleaved: bool = False, stream=None):
+    """sr_page_append_norm: page_append with norms of the query and key heads
+    (gains q_norm, k_norm float [hd]; None: no norm), into pools of float, bf16 or
+    4 bits (uint8 [n_pages][hkv][page_tokens][fp4_token_bytes(hd)])."""
+    import torch
+    f32 = torch.float32
+    cache, rows, mp, hkv, pt, hd, n_pages = _any_layer_args(kpool, vpool, table, lens, n_new)
+    _, lr, hq, _ = _sizes(q, "q", (f32,), 4)
+    _expect(q, "q", f32, (rows, lr, hq, hd))
+    _expect(qkv, "qkv", f32, (rows, lr, (hq + 2 * hkv) * hd))
+    rot = 0 if freqs is None else 2 * _sizes(freqs, "freqs", (torch.float64,), 1)[0]
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None:
+            _expect(t, name, f32, (hd,))
+    _run((qkv, freqs, table, lens, kpool, vpool, q, n_new, q_norm, k_norm), stream, lib().sr_page_append_norm,
+         (cache, hd, hq, hkv, rows, lr, qkv.data_ptr(), _ptr(freqs), rot, 1 if interleaved else 0, _ptr(q_norm), _ptr(k_norm),
+          eps, kpool.data_ptr(), vpool.data_ptr(), pt, n_pages, table.data_ptr(), mp, lens.data_ptr(), _ptr(n_new),
+          q.data_ptr()))
+
+
+def page_read(kpool, vpool, table, lens, k_out=None, v_out=None, n_new=None, stream=None):
+    """sr_page_read: the rows' last tokens as the pages (float, bf16 or 4 bits) hold
+    them -> k_out, v_out float or bf16 [rows][lr][hkv][hd]; either may be None."""
+    import torch
+    cache, rows, mp, hkv, pt, hd, n_pages = _any_layer_args(kpool, vpool, table, lens, n_new)
+    one = k_out if k_out is not None else v_out
+    if one is None:
+        raise ValueError("no output")
+    _, lr, _, _ = _sizes(one, "k_out" if k_out is not None else "v_out", _cache_types(), 4)
+    for t, pool, name in ((k_out, kpool, "k_out"), (v_out, vpool, "v_out")):
+        if t is not None:
+            _expect(t, name, one.dtype, (rows, lr, hkv, hd))
+            if pool is None:
+                raise ValueError(f"{name} without its pool")
+    _run((one, k_out, v_out, kpool, vpool, table, lens, n_new), stream, lib().sr_page_read,
+         (cache, SR_F32 if one.dtype is torch.float32 else SR_BF16, hd, hkv, rows, lr, _ptr(kpool), _ptr(vpool), pt, n_pages,
+          table.data_ptr(), mp, lens.data_ptr(), _ptr(n_new), _ptr(k_out), _ptr(v_out)))
+
+
+def paged_attention_fp4(q, kpool, vpool, table, lens, out, n_new=None, window: int = 0, sinks: int = 0, shared: int = 0,
+                        max_len: int = None, stream=None):
+    """sr_paged_attention_fp4: paged_attention over one layer's pools of 4 bits
+    (uint8 [n_pages][hkv][page_tokens][fp4_token_bytes(hd)]); out [rows][lr][hq*hd]
+    in bf16 (may travel as int16) or float."""
+    import torch
+    if kpool.dtype is not torch.uint8:
+        raise ValueError(f"kpool: expected torch.uint8 pages of 4 bits, got {kpool.dtype}")
+    _, rows, mp, hkv, pt, hd, n_pages = _any_layer_args(kpool, vpool, table, lens, n_new)
+    _, lr, hq, _ = _sizes(q, "q", (torch.float32,), 4)
+    _expect(q, "q", torch.float32, (rows, lr, hq, hd))
+    if out.dtype not in _cache_types():
+        raise ValueError(f"out has type {out.dtype}")
+    _expect(out, "out", out.dtype, (rows, lr, hq * hd))
+    dtype = SR_F32 if out.dtype is torch.float32 else SR_BF16
+    if max_len is None:
+        max_len = max(1, mp * pt)
+    _int32(window, sinks, shared, max_len)
+    L = lib()
+    _run((q, kpool, vpool, table, lens, out, n_new), stream, L.sr_paged_attention_fp4,
+         (dtype, hd, hq, hkv, rows, lr, q.data_ptr(), kpool.data_ptr(), vpool.data_ptr(), pt, n_pages, table.data_ptr(), mp,
+          lens.data_ptr(), _ptr(n_new), window, sinks, shared, max_len, out.data_ptr()),
+         L.sr_paged_attention_fp4_scratch(dtype, hd, hq, hkv, rows, lr, pt, mp, window, sinks, shared, max_len),
+         torch.float32, 20)
+
+
+def sample_filtered(logits, random, tokens, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None,
+                    stream=None):
+    """sr_sample_filtered: logits [rows][vocab] (rows may be strided; float or bf16,
+    which may travel as int16) and random words int32 [rows] (may be strided, as a
+    column of philox_fill's) -> tokens int32 [rows], logprob float [rows], kept
+    int32 [rows]; any output may be None.  Each setting is a number for every row
+    or a tensor [rows] (top_k int32, the others float)."""
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    if logits.dtype not in _cache_types() or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: type {logits.dtype}, shape {tuple(logits.shape)}, strides {logits.stride()}")
+    rows, vocab = logits.shape
+    if random.dtype is not i32 or random.shape != (rows,):
+        raise ValueError(f"random: expected torch.int32 of shape {(rows,)}, got {random.dtype}, {tuple(random.shape)}")
+    each, same = [], []
+    for v, name, typ in ((temperature, "temperature", f32), (top_k, "top_k", i32), (top_p, "top_p", f32), (min_p, "min_p", f32)):
+        if torch.is_tensor(v):
+            _expect(v, name, typ, (rows,))
+        elif typ is i32:
+            if int(v) != v:
+                raise ValueError(f"{name}: expected a whole number, got {v}")
+            _int32(int(v))
+        each.append(v if torch.is_tensor(v) else None)
+        same.append(0 if torch.is_tensor(v) else int(v) if typ is i32 else v)
+    for t, name, typ in ((tokens, "tokens", i32), (logprob, "logprob", f32), (kept, "kept", i32)):
+        if t is not None:
+            _expect(t, name, typ, (rows,))
+    _int32(rows, vocab)
+    stride = logits.stride(0) if rows > 1 else vocab
+    L = lib()
+    _run((logits, random, tokens, logprob, kept, *each), stream, L.sr_sample_filtered,
+         (SR_F32 if logits.dtype is f32 else SR_BF16, logits.data_ptr(), stride, rows, vocab, _ptr(each[0]), same[0],
+          _ptr(each[1]), same[1], _ptr(each[2]), same[2], _ptr(each[3]), same[3], random.data_ptr(),
+          random.stride(0) if rows > 1 else 1, _ptr(tokens), _ptr(logprob), _ptr(kept)),
+         L.sr_sample_filtered_scratch(rows, vocab), i32, 18)

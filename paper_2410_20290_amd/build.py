@@ -1,8 +1,8 @@
 """Build libspecrej.so (HIP for gfx950) in-tree with hipcc.
 
 Every translation unit is compiled with packed-fp32 instruction selection
-off; the sampler additionally with floating-point contraction off, because
-its float32 steps must round exactly as specified.
+off; the samplers additionally with floating-point contraction off, because
+their float32 steps must round exactly as specified.
 """
 import os
 import subprocess
@@ -14,12 +14,13 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspecrej.so")
 SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "sampler.hip", "cut.hip", "pages.hip", "paged_attention.hip",
-           "logprobs.hip", "host.cpp", "ops.cpp", "diagnostics.cpp"]
+           "logprobs.hip", "page_norm.hip", "paged_attention_fp4.hip", "filtered.hip", "host.cpp", "ops.cpp", "serving.cpp",
+           "diagnostics.cpp"]
 ARCH = "gfx950"
 COMMON = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-I", os.path.join(HERE, "..", "include")]
-EXTRA = {"sampler.hip": ["-ffp-contract=off"]}
+EXTRA = {"sampler.hip": ["-ffp-contract=off"], "filtered.hip": ["-ffp-contract=off"]}
 
 
 def _compile(src: str) -> str:

@@ -216,6 +216,7 @@ struct PagePool {
   void* pool;
   int64_t block_bytes;
   int n_layers, hkv, row_bytes, shift, n_pages;   // row_bytes: one key of one head
+  bool mixed;   // a page's tokens are not runs of row_bytes (codes, then scales): copied whole
 };
 struct PageReserveArgs {
   PagePool p;
@@ -266,6 +267,55 @@ struct PagedAttnArgs {
 };
 size_t paged_attn_scratch(const PagedAttnArgs& a);
 void paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+// ---- caches of 4 bits and the filtered draw (see specrej_serving.h) ----------
+struct PageAppendNormArgs {
+  PageAppendArgs a;               // dtype: the cache's (SR_FP4 too)
+  const float *q_gain, *k_gain;   // or null: no norm
+  double eps;
+};
+void page_append_norm(const PageAppendNormArgs& a, hipStream_t s);
+
+struct PageReadArgs {
+  int cache, dtype, hd, hkv, rows, lr;
+  const void *kpool, *vpool;
+  int shift, n_pages;
+  const int32_t* table;
+  int max_pages;
+  const int32_t *lens, *n_new;
+  void *k_out, *v_out;
+};
+void page_read(const PageReadArgs& a, hipStream_t s);
+
+// dtype: the output's; the pools hold 4 bits.
+size_t paged_attn_fp4_scratch(const PagedAttnArgs& a);
+void paged_attn_fp4(const PagedAttnArgs& a, hipStream_t s);
+
+// One number for every row, or one each.
+template <typename T>
+struct PerRow {
+  const T* each;
+  T all;
+#ifdef __HIPCC__
+  __device__ T operator[](int r) const { return each ? each[r] : all; }
+#endif
+};
+struct FilteredArgs {
+  int dtype;
+  const void* logits;
+  int64_t row_stride;
+  int rows, vocab;
+  PerRow<float> temperature, top_p, min_p;
+  PerRow<int32_t> top_k;
+  const uint32_t* random;
+  int64_t random_stride;
+  int32_t* token;
+  float* logprob;
+  int32_t* kept;
+  uint32_t* scratch;
+};
+size_t sample_filtered_scratch(int rows, int vocab);
+void sample_filtered(const FilteredArgs& a, hipStream_t s);
 
 // ---- log-probabilities of given tokens (see specrej_ops.h) -------------------
 struct LogprobArgs {

@@ -353,7 +353,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(PageReserveA
 }
 
 // The new entries, lengths and counts (a wave per row), then the copies (a
-// wave per page, block and head: one run of filled slots).
+// wave per page, block and head: one run of filled slots, or all of a page whose
+// tokens are not runs).
 __global__ void __launch_bounds__(256) reserve_apply_kernel(PageReserveArgs a) {
   const ReservePlan pl = reserve_plan(a.scratch, a.rows);
   const int lane = threadIdx.x & 63;
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(256) reserve_apply_kernel(PageReserveArgs a) {
     char* base = (char*)a.p.pool + blk * a.p.block_bytes;
     const uint4* src = reinterpret_cast<const uint4*>(base + ((int64_t)pl.src[i] * hkv + h) * run);
     uint4* dst = reinterpret_cast<uint4*>(base + ((int64_t)pl.free[pl.at[i]] * hkv + h) * run);
-    const int n = pl.part[i] * row16;
+    const int n = a.p.mixed ? (int)(run >> 4) : pl.part[i] * row16;
     for (int k = lane; k < n; k += 64) dst[k] = src[k];
   }
 }

@@ -1,0 +1,195 @@
+"""The operators of specrej_serving.h on the CPU: every declared symbol is
+exported, the header is plain C, bad arguments are refused with the documented
+status before any device work, the binding checks its tensors, and the tests' own
+4-bit format is right on values worked by hand."""
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+
+import fp4_util
+import paper_2410_20290_amd as sr
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INVALID, SMALL, UNSUPPORTED = sr.SR_ERR_INVALID_ARG, sr.SR_ERR_WORKSPACE_TOO_SMALL, sr.SR_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(sr.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return sr.lib()
+
+
+def test_header_symbols_exported(L):
+    text = open(os.path.join(ROOT, "include", "specrej_serving.h")).read()
+    names = sorted(set(re.findall(r"^(?:sr_status|size_t)\s+(sr_\w+)\(", text, re.M)))
+    assert len(names) == 6, names
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def test_header_is_plain_c(tmp_path):
+    src = tmp_path / "t.c"
+    src.write_text('#include "specrej_serving.h"\nint main(void) { return SR_FP4; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-fsyntax-only", "-I", os.path.join(ROOT, "include"), str(src)],
+                   check=True)
+
+
+def args(defaults, kw):
+    d = dict(defaults)
+    assert set(kw) <= set(d)
+    d.update(kw)
+    return list(d.values())
+
+
+APPEND = dict(cache=sr.SR_FP4, hd=64, hq=8, hkv=2, rows=2, lr=3, qkv=0x100000, freqs=0x200000, rot=64, inter=0, gq=0x210000,
+              gk=0x220000, eps=1e-5, k=0x300000, v=0x400000, pt=16, n_pages=8, table=0x500000, mp=4, lens=0x600000, new=None,
+              q=0x700000, stream=None)
+LAYER_BAD = [
+    (dict(hd=48), UNSUPPORTED), (dict(hd=256), UNSUPPORTED), (dict(hkv=0), INVALID), (dict(rows=-1), INVALID),
+    (dict(lr=-1), INVALID), (dict(pt=20), UNSUPPORTED), (dict(mp=0), INVALID), (dict(n_pages=0), INVALID), (dict(k=None), INVALID),
+    (dict(v=None), INVALID), (dict(table=None), INVALID), (dict(lens=None), INVALID), (dict(k=0x300008), INVALID),
+    (dict(v=0x400002), INVALID), (dict(rows=4097), UNSUPPORTED), (dict(n_pages=(1 << 20) + 1), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("kw,status", LAYER_BAD + [
+    (dict(cache=3), INVALID), (dict(cache=-1), INVALID), (dict(hq=7), INVALID), (dict(q=None), INVALID), (dict(q=0x700004), INVALID),
+    (dict(qkv=None), INVALID), (dict(qkv=0x100008), INVALID), (dict(rot=65), INVALID), (dict(rot=72), INVALID),
+    (dict(rot=12), INVALID), (dict(rot=-8), INVALID), (dict(freqs=None), INVALID), (dict(v=0x300000), INVALID),
+    (dict(v=0x300000 + 8 * 2 * 16 * 34 - 16), INVALID), (dict(q=0x100000), INVALID), (dict(q=0x300000), INVALID),
+    (dict(gq=0x700000), INVALID), (dict(gk=0x300010), INVALID), (dict(eps=-1e-9), INVALID), (dict(eps=float("nan")), INVALID),
+    (dict(eps=float("inf")), INVALID), (dict(rows=4096, lr=4096), UNSUPPORTED)])
+def test_append_norm_refuses(L, kw, status):
+    assert L.sr_page_append_norm(*args(APPEND, kw)) == status and sr.last_error()
+
+
+READ = dict(cache=sr.SR_FP4, dtype=sr.SR_BF16, hd=64, hkv=2, rows=2, lr=3, k=0x300000, v=0x400000, pt=16, n_pages=8,
+            table=0x500000, mp=4, lens=0x600000, new=None, ko=0x700000, vo=0x800000, stream=None)
+
+
+@pytest.mark.parametrize("kw,status", LAYER_BAD + [
+    (dict(cache=4), INVALID), (dict(dtype=2), INVALID), (dict(ko=0x700008), INVALID), (dict(vo=0x700000), INVALID),
+    (dict(ko=0x300000), INVALID), (dict(vo=0x500000), INVALID), (dict(rows=4096, lr=4096), UNSUPPORTED)])
+def test_read_refuses(L, kw, status):
+    assert L.sr_page_read(*args(READ, kw)) == status and sr.last_error()
+
+
+ATTN = dict(dtype=sr.SR_BF16, hd=64, hq=8, hkv=2, rows=2, lr=3, q=0x700000, k=0x300000, v=0x400000, pt=16, n_pages=8,
+            table=0x500000, mp=4, lens=0x600000, new=None, window=0, sinks=0, shared=0, max_len=64, out=0x800000,
+            scratch=0x10000000, n=1 << 22, stream=None)
+
+
+@pytest.mark.parametrize("kw,status", LAYER_BAD + [
+    (dict(dtype=2), INVALID), (dict(hq=7), INVALID), (dict(q=None), INVALID), (dict(q=0x700004), INVALID),
+    (dict(hq=34), UNSUPPORTED), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID), (dict(shared=-1), INVALID),
+    (dict(max_len=0), INVALID), (dict(out=None), INVALID), (dict(out=0x800002), INVALID), (dict(out=0x700000), INVALID),
+    (dict(out=0x300000), INVALID), (dict(rows=4096, lr=1 << 16), UNSUPPORTED)])
+def test_attention_refuses(L, kw, status):
+    assert L.sr_paged_attention_fp4(*args(ATTN, kw)) == status and sr.last_error()
+
+
+def test_nothing_to_do(L):
+    for kw in (dict(rows=0), dict(lr=0)):
+        assert L.sr_page_append_norm(*args(APPEND, kw)) == sr.SR_OK and sr.last_error() == ""
+        assert L.sr_page_read(*args(READ, kw)) == sr.SR_OK
+        assert L.sr_paged_attention_fp4(*args(ATTN, kw)) == sr.SR_OK
+    assert L.sr_page_read(*args(READ, dict(ko=None, vo=None))) == sr.SR_OK
+    assert L.sr_paged_attention_fp4_scratch(9, 64, 8, 2, 1, 1, 16, 4, 0, 0, 0, 64) == 0
+    assert L.sr_sample_filtered(*args(DRAW, dict(rows=0))) == sr.SR_OK
+
+
+DRAW = dict(dtype=sr.SR_F32, logits=0x100000, stride=1000, rows=2, vocab=1000, T=None, T_all=1.0, k=None, k_all=0, p=None, p_all=1.0,
+            m=None, m_all=0.0, random=0x200000, rstride=1, token=0x300000, lp=0x400000, kept=0x500000, scratch=0x10000000,
+            n=1 << 24, stream=None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), INVALID), (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(stride=999), INVALID),
+    (dict(vocab=262145, stride=262145), UNSUPPORTED), (dict(rows=(1 << 20) + 1), UNSUPPORTED), (dict(logits=None), INVALID),
+    (dict(random=None), INVALID), (dict(rstride=-1), INVALID), (dict(logits=0x100002), INVALID), (dict(T=0x600002), INVALID),
+    (dict(k=0x600001), INVALID), (dict(token=0x100000), INVALID), (dict(lp=0x300004), INVALID), (dict(kept=0x200004), INVALID),
+    (dict(token=0x600000, T=0x600004), INVALID), (dict(lp=0x600000, m=0x600000), INVALID), (dict(stride=(1 << 40) + 1), UNSUPPORTED)])
+def test_draw_refuses(L, kw, status):
+    assert L.sr_sample_filtered(*args(DRAW, kw)) == status and sr.last_error()
+
+
+def test_pools_of_four_bits(L):
+    """sr_page_reserve and sr_page_compact with elem_bytes 1."""
+    base = dict(pool=0x1000000, block=64 * 2 * 16 * 34, nl=2, hkv=2, hd=34, eb=1, pt=16, n_pages=64, table=0x10000,
+                lens=0x20000, refs=0x30000, rows=4, mp=8, add=None, add_all=1, to=0x40000, lo=0x50000, ro=0x60000,
+                granted=0x70000, info=0x80000, scratch=0x90000, n=1 << 20, stream=None)
+    for kw, status in ((dict(hd=64), UNSUPPORTED), (dict(hd=16), UNSUPPORTED), (dict(block=64 * 2 * 16 * 34 - 16), INVALID),
+                       (dict(block=64 * 2 * 16 * 34 + 8), UNSUPPORTED), (dict(info=0x1000000), INVALID)):
+        assert L.sr_page_reserve(*args(base, kw)) == status and sr.last_error()
+        comp = {k: v for k, v in base.items() if k not in ("add", "add_all", "lo", "granted")}
+        assert L.sr_page_compact(*args(comp, kw)) == status
+
+
+def test_binding_checks_tensors():
+    """Wrong types, shapes, layouts and devices raise before the library is called."""
+    import torch
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    f = lambda *s: torch.zeros(s)  # noqa: E731
+    k = torch.zeros((8, 2, 16, 34), dtype=torch.uint8)
+    good = dict(q=f(3, 2, 8, 64), kpool=k, vpool=k.clone(), table=i(3, 4), lens=i(3), out=torch.zeros((3, 2, 512), dtype=torch.bfloat16))
+    for bad in (dict(q=f(3, 2, 8, 32)), dict(q=f(4, 2, 8, 64)), dict(vpool=k.float()), dict(out=f(3, 2, 511)),
+                dict(out=torch.zeros((3, 2, 512), dtype=torch.float16)), dict(n_new=i(2)), dict(kpool=k[:, :1]), dict(kpool=f(8, 2, 16, 64)),
+                dict(kpool=torch.zeros((8, 2, 16, 33), dtype=torch.uint8)), dict(kpool=k[..., ::2])):
+        with pytest.raises(ValueError):
+            sr.paged_attention_fp4(**{**good, **bad})
+    with pytest.raises(ValueError, match="GPU"):
+        sr.paged_attention_fp4(**good)
+    for kw in (dict(window=2 ** 32 + 5), dict(sinks=2 ** 31), dict(shared=-2 ** 40), dict(max_len=2 ** 32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            sr.paged_attention_fp4(**good, **kw)
+    for pool, hd in ((k, 64), (f(8, 2, 16, 64), 64), (torch.zeros((8, 2, 16, 32), dtype=torch.bfloat16), 32)):
+        good = dict(qkv=f(3, 2, 12 * hd), freqs=f(hd // 2).double(), table=i(3, 4), lens=i(3), kpool=pool, vpool=pool.clone(),
+                    q=f(3, 2, 8, hd), q_norm=f(hd), k_norm=f(hd))
+        for bad in (dict(qkv=f(3, 2, 11 * hd)), dict(freqs=f(hd // 2)), dict(q_norm=f(hd + 1)), dict(k_norm=f(hd).double()),
+                    dict(vpool=pool.double()), dict(n_new=i(4)), dict(q=f(3, 2, 8, 2 * hd))):
+            with pytest.raises(ValueError):
+                sr.page_append_norm(**{**good, **bad})
+        with pytest.raises(ValueError, match="GPU"):
+            sr.page_append_norm(**good)
+        good = dict(kpool=pool, vpool=pool, table=i(3, 4), lens=i(3), k_out=f(3, 2, 2, hd), v_out=f(3, 2, 2, hd))
+        for bad in (dict(k_out=f(3, 2, 2, hd + 1)), dict(v_out=f(3, 2, 2, hd).bfloat16()), dict(k_out=None, v_out=None), dict(kpool=None),
+                    dict(kpool=None, vpool=None), dict(k_out=f(3, 2, 2, hd).double())):
+            with pytest.raises(ValueError):
+                sr.page_read(**{**good, **bad})
+        with pytest.raises(ValueError, match="GPU"):
+            sr.page_read(**good)
+    good = dict(logits=f(3, 9), random=i(3), tokens=i(3), logprob=f(3), kept=i(3))
+    for bad in (dict(logits=f(9, 3).t()), dict(logits=f(3, 9).double()), dict(tokens=i(2)), dict(random=i(3).long()), dict(random=i(4)),
+                dict(logprob=f(4)), dict(kept=f(3)), dict(temperature=i(3)), dict(top_k=f(3)), dict(top_p=f(2)), dict(top_k=1.5),
+                dict(top_k=2 ** 32 + 5), dict(min_p=f(3, 1))):
+        with pytest.raises(ValueError):
+            sr.sample_filtered(**{**good, **bad})
+    with pytest.raises(ValueError, match="GPU"):
+        sr.sample_filtered(**good)
+    with pytest.raises(ValueError):
+        sr.fp4_token_bytes(48)
+    assert [sr.fp4_token_bytes(n) for n in (32, 64, 128)] == [17, 34, 68]
+
+
+def test_the_plain_format():
+    x = np.zeros(32)
+    x[:10] = [0.25, 0.75, -1.25, 1.75, 2.5, -3.5, 5.0, 6.9, 0.26, -0.0]
+    codes, scales = fp4_util.quantise(x)
+    assert scales.tolist() == [127] and codes[:10].tolist() == [0, 2, 10, 4, 4, 14, 6, 7, 1, 8]
+    assert fp4_util.dequantise(codes, scales)[:9].tolist() == [0, 1, -1, 2, 2, -4, 4, 6, 0.5]
+    for top, b in ((6.999, 127), (7.0, 128), (3.499, 126), (3.5, 127), (0.0, 2), (1e-45, 2), (2.0 ** 127, 252), (3.4e38, 252),
+                   (np.inf, 255), (np.nan, 255)):
+        x[7] = top
+        x[:7] = 0.0
+        x[8:] = 0.0
+        codes, scales = fp4_util.quantise(x)
+        assert scales.tolist() == [b], (top, scales)
+        assert (codes == 0).all() == (b == 255 or top < 1e-40)
+    raw = fp4_util.pack(np.arange(2 * 32).reshape(1, 1, 2, 32).astype(np.uint8) & 15, np.array([5, 9], np.uint8).reshape(1, 1, 2, 1))
+    assert raw.shape == (1, 1, 2, 17) and raw.ravel()[:4].tolist() == [0x10, 0x32, 0x54, 0x76] and raw.ravel()[-2:].tolist() == [5, 9]
+    codes, scales = fp4_util.unpack(raw)
+    assert codes.ravel()[:20].tolist() == [i & 15 for i in range(20)] and scales.ravel().tolist() == [5, 9]
