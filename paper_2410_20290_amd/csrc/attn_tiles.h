@@ -33,8 +33,15 @@ __device__ __forceinline__ uint32_t lds_addr(const bf16_t* p) {
 // (vmcnt 0), they leave the next tile's copies flying.
 template <int N, int LO, int HI>
 __device__ __forceinline__ void lds_read_tr16_pairs(const uint32_t (&a)[N], i16x4 (&lo)[N], i16x4 (&hi)[N]) {
-  static_assert(N == 2 || N == 4, "pairs");
-  if constexpr (N == 2) {
+  static_assert(N == 1 || N == 2 || N == 4, "pairs");
+  if constexpr (N == 1) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(lo[0]), "=&v"(hi[0])
+        : "v"(a[0]), "n"(LO), "n"(HI)
+        : "memory");
+  } else if constexpr (N == 2) {
     asm volatile(
         "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
         "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
