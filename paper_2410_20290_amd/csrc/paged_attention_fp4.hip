@@ -29,6 +29,8 @@
 
 namespace sr {
 
+constexpr float kStale = 8.f;
+
 // Eight codes (a word, the lowest first) times a scale, as bf16.
 __device__ __forceinline__ bf16x8 fp4_to_bf16(uint32_t w, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
@@ -46,6 +48,20 @@ __device__ __forceinline__ void in_parts(float x, __bf16 (&p)[P]) {
     p[i] = (__bf16)x;
     x -= (float)p[i];
   }
+}
+
+// The sum over the lanes that hold a column's parts, the same bits in each of them
+// (rotations by 8, then 4 of 16 lanes: every addition is of the same pair in both of
+// its lanes), or their probabilities' parts would not fit together.
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int SPREAD>
+__device__ __forceinline__ float parts_sum(float v) {
+  if constexpr (SPREAD > 1) v += rotated<0x128>(v);
+  if constexpr (SPREAD == 4) v += rotated<0x124>(v);
+  return v;
 }
 
 // N 4-byte words from an address aligned to them.
@@ -71,6 +87,26 @@ __device__ __forceinline__ int wslot(int k, int c) {
 }
 
 // ------------------------------------------------------- waves split keys
+// Query columns of a work-group and where their parts go: with up to 8 (4) columns each
+// is there SPREAD = 2 (4) times, and the matrix columns hold a part each, at no
+// product more; else every part takes products of its own.
+template <bool F32, int SPREAD>
+struct Fp4Parts {
+  static constexpr int COLS = 16 / SPREAD;
+  static constexpr int SETS = SPREAD > 1 ? 1 : F32 ? 3 : 2;   // products of a score
+  static constexpr int PSETS = !F32 || SPREAD > 1 ? 1 : 3;    // of a value
+};
+// Part `part` of P parts of x, 0 beyond them.
+template <int SPREAD, int P>
+__device__ __forceinline__ __bf16 my_part(float x, int part) {
+  __bf16 p[P];
+  in_parts<P>(x, p);
+  __bf16 r = p[0];
+#pragma unroll
+  for (int i = 1; i < SPREAD; ++i) r = part == i ? (i < P ? p[i < P ? i : 0] : (__bf16)0.f) : r;
+  return r;
+}
+
 // At most 16 query columns: column x is token x / G of the row's, query head x % G of
 // the KV head's G.  Work-group = (split, KV head, row), NW waves; every wave takes an
 // even share of the 32-key blocks that hold visible keys and waits on no other until
@@ -78,19 +114,19 @@ __device__ __forceinline__ int wslot(int k, int c) {
 //   S^T = K Q^T   (v_mfma_f32_16x16x32_bf16): a lane takes HD / 4 neighbouring
 //         dimensions of a key, one load of codes and one scale, and converts them
 //         in its registers; the contraction visits dimensions in that order.
-//   O^T += V^T P^T: a V block is converted on its way into LDS (the wave's own) and
-//         its A operand comes from two transpose reads; the contraction visits the
-//         keys in the order the lane holds their probabilities.
-// The next block's codes are in flight while one is computed.  A block's 16-key
-// halves lie in one page each; lane i holds the page numbers of block i of a run
-// of 64.  The keys below common[row] are another pass's.  Keys that nobody sees are
-// read where they lie (their scores are masked) and their values as zeros; a half
-// without a page is read from page 0.
-template <int HD, int NW, bool F32>
-__global__ void __launch_bounds__(64 * NW)
+//   O^T += V^T P^T (v_mfma_f32_16x16x32_bf16): a V block is converted on its way into
+//         LDS (the wave's own) and its A operand comes from two transpose reads; the
+//         contraction visits the keys in the order the lane holds their probabilities.
+// A block's registers take over the next block as soon as they are read.  A block's 16-key halves lie in one page each; lane i holds
+// the places and flags of block i of a run of 64.  The keys below common[row] are
+// another pass's.  Keys that nobody sees are read where they lie (their scores are
+// masked) and their values as zeros; a half without a page is read from page 0.
+template <int HD, int NW, bool F32, int SPREAD>
+__global__ void __launch_bounds__(64 * NW, HD == 128 && SPREAD == 1 ? 3 : 4)
 fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
+  typedef Fp4Parts<F32, SPREAD> PT;
+  constexpr int COLS = PT::COLS, SETS = PT::SETS, PSETS = PT::PSETS;
   constexpr int KS = HD / 32, DT = HD / 16, CPK = HD / 8, VB = 32 * HD;
-  constexpr int QP = F32 ? 3 : 2, PP = F32 ? 3 : 1;
   // values: lanes of a key, loads of a block, words of a load
   constexpr int LPV = HD == 128 ? 4 : 2, NV = HD == 128 ? 2 : 1, WV = HD == 32 ? 2 : 4;
   constexpr int ROW = HD + 4;                       // floats of a column in the merge
@@ -103,7 +139,8 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fg = lane >> 4;
   const int g = a.hq / a.hkv;
-  const int t = fr / g;                             // this lane's column
+  const int col = fr % COLS, part = fr / COLS;      // this lane's column, and which part of it
+  const int t = col / g;
   const bool live = t < rs.n;
   const int end_c = rs.p0 + (live ? t : 0) + 1, lo_c = window_start(end_c - 1, a.window);
   const int lo_last = window_start(rs.len - 1, a.window);
@@ -115,71 +152,95 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   const int mask = (1 << a.shift) - 1;
   bf16_t* vbuf = lds + wave * VB;
 
-  // The pages of blocks [base, base + 64) of this wave, -1 for none.
-  int base = i0, d0 = -1, d1 = -1;
+  // Blocks [base, base + 64) of this wave: lane i holds block base + i's places (the
+  // pages' blocks of the KV head, in units of 16 bytes) and flags.
+  enum {
+    GONE0 = 1, GONE1 = 2,   // no page holds the half
+    EDGE = 4,               // some column does not see some key
+    PARTLY = 8              // nobody sees some key
+  };
+  int base = i0;
+  uint32_t flags = 0;
+  uint32_t place[2];   // (16 bytes of a layer's block: below 2^32 of them, 64 GB a layer, as the entry point checks)
   auto look_up = [&] {
-    d0 = d1 = -1;
+    flags = EDGE | PARTLY | GONE0 | GONE1;
+    place[0] = place[1] = 0;
     if (base + lane < i1) {
       const int k0 = kb.key0(base + lane);
       const int p0 = kb.any16(k0) ? tab[k0 >> a.shift] : -1;
       const int p1 = kb.any16(k0 + 16) ? tab[(k0 + 16) >> a.shift] : -1;
-      d0 = (uint32_t)p0 < (uint32_t)a.n_pages ? p0 : -1;
-      d1 = (uint32_t)p1 < (uint32_t)a.n_pages ? p1 : -1;
+      const bool ok0 = (uint32_t)p0 < (uint32_t)a.n_pages, ok1 = (uint32_t)p1 < (uint32_t)a.n_pages;
+      flags = (ok0 ? 0 : GONE0) | (ok1 ? 0 : GONE1);
+      if (flags || !kb.all32(k0)) flags |= PARTLY;
+      if (flags || k0 + 32 > rs.p0 + 1 || (k0 < lo_last && k0 + 32 > a.sinks)) flags |= EDGE;
+      if (ok0) place[0] = (uint32_t)(fp4_block(p0, a.hkv, h, a.shift, HD) >> 4);
+      if (ok1) place[1] = (uint32_t)(fp4_block(p1, a.hkv, h, a.shift, HD) >> 4);
     }
   };
   struct Block {
     uint32_t k[2][KS], v[NV][WV];
     uint8_t ks[2], vs[NV];
-  };
-  auto load_block = [&](int b, Block& x) {
-    const int pg[2] = {__builtin_amdgcn_readlane(d0, b), __builtin_amdgcn_readlane(d1, b)};
-    const int k0 = kb.key0(base + b);
-    int64_t blk[2];
-    int slot[2];
+  } x;
+  const uint32_t kcodes = fr * (HD / 2) + fg * (HD / 8), kscale = fr * KS + fg * (HD / 4) / 32;
+  // (the place of a half of block b, and its first slot)
+  auto half_at = [&](int b, int u) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place[u], b) << 4; };
+  auto half_slot = [&](int b, int u) { return (kb.key0(base + b) + 16 * u) & mask; };
+  auto load_keys = [&](int b) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      blk[u] = fp4_block(imax(pg[u], 0), a.hkv, h, a.shift, HD);
-      slot[u] = (k0 + 16 * u) & mask;
-      const uint8_t* src = (const uint8_t*)a.kpool + blk[u];
-      load_words<KS>(src + fp4_codes(slot[u], HD) + (fr * (HD / 2) + fg * (HD / 8)), x.k[u]);
-      x.ks[u] = (src + fp4_scales(slot[u], a.shift, HD))[fr * KS + fg * (HD / 4) / 32];
+      const uint8_t* src = (const uint8_t*)a.kpool + half_at(b, u);
+      const int slot = half_slot(b, u);
+      load_words<KS>(src + fp4_codes(slot, HD) + kcodes, x.k[u]);
+      x.ks[u] = (src + fp4_scales(slot, a.shift, HD))[kscale];
     }
+  };
+  auto load_values = [&](int b) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int kk = i * (64 / LPV) + lane / LPV, c = lane % LPV;
-      const int u = NV == 2 ? i : 0;
-      int64_t at = blk[u];
-      int s = slot[u];
-      if (NV == 1 && lane >= 32) {
-        at = blk[1];
-        s = slot[1];
+      uint64_t from = half_at(b, NV == 2 ? i : 0);
+      int s = half_slot(b, NV == 2 ? i : 0);
+      if (NV == 1) {
+        const uint64_t from1 = half_at(b, 1);
+        const int s1 = half_slot(b, 1);
+        if (lane >= 32) {
+          from = from1;
+          s = s1;
+        }
       }
-      const uint8_t* src = (const uint8_t*)a.vpool + at;
+      const uint8_t* src = (const uint8_t*)a.vpool + from;
       load_words<WV>(src + fp4_codes(s, HD) + ((kk & 15) * (HD / 2) + c * 4 * WV), x.v[i]);
       x.vs[i] = (src + fp4_scales(s, a.shift, HD))[(kk & 15) * KS + c * WV / 4];
     }
   };
 
   // The first block's loads go out before the queries are read.
-  Block xa, xb;
-  look_up();
-  if (i0 < i1) load_block(0, xa);
+  auto start = [&] {
+    look_up();
+    load_keys(0);
+    load_values(0);
+  };
+  if (i0 < i1) start();
 
-  // Q^T fragments (B operand): lane holds Q[column fr][HD / 4 fg + 8 s .. + 8]
-  bf16x8 qf[QP][KS];
+  // Q^T fragments (B operand): lane holds Q[its column][HD / 4 fg + 8 s .. + 8]
+  bf16x8 qf[SETS][KS];
   {
-    const float* qr = a.q + (((int64_t)row * a.lr + (live ? t : 0)) * a.hq + h * g + (live ? fr - t * g : 0)) * HD;
+    const float* qr = a.q + (((int64_t)row * a.lr + (live ? t : 0)) * a.hq + h * g + (live ? col - t * g : 0)) * HD;
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
-      const float4 x = *reinterpret_cast<const float4*>(qr + HD / 4 * fg + 8 * st);
-      const float4 y = *reinterpret_cast<const float4*>(qr + HD / 4 * fg + 8 * st + 4);
-      const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      const float4 x4 = *reinterpret_cast<const float4*>(qr + HD / 4 * fg + 8 * st);
+      const float4 y4 = *reinterpret_cast<const float4*>(qr + HD / 4 * fg + 8 * st + 4);
+      const float v[8] = {x4.x, x4.y, x4.z, x4.w, y4.x, y4.y, y4.z, y4.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        __bf16 p[QP];
-        in_parts<QP>(v[e] * qscale, p);
+        if constexpr (SPREAD > 1) {
+          qf[0][st][e] = my_part<SPREAD, F32 ? 3 : 2>(v[e] * qscale, part);
+        } else {
+          __bf16 p[SETS];
+          in_parts<SETS>(v[e] * qscale, p);
 #pragma unroll
-        for (int i = 0; i < QP; ++i) qf[i][st][e] = p[i];
+          for (int i = 0; i < SETS; ++i) qf[i][st][e] = p[i];
+        }
       }
     }
   }
@@ -187,34 +248,21 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   f32x4 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  // from the lowest finite score: while a column has seen only -inf its
+  // probabilities are exp2(-inf) = 0, where -inf - -inf would be NaN
+  float m = -FLT_MAX, l = 0.f;
   // transpose-read addresses: lane names 4 dims (dt 16 + 4 (fr & 3) ..) of key
   // 4 fg + (fr >> 2), and of the key 16 on (16 rows on, same slots)
-  uint32_t vaddr[DT];
+  // (slots differ from dt to dt by an exclusive or: they stay within aligned rows)
+  uint32_t vaddr;
   {
     const int kr0 = 4 * fg + (fr >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      vaddr[dt] = lds_addr(vbuf + kr0 * HD + 8 * wslot<CPK>(kr0, 2 * dt + ((fr & 3) >> 1)) + 4 * (fr & 1));
+    vaddr = lds_addr(vbuf + kr0 * HD + 8 * wslot<CPK>(kr0, (fr & 3) >> 1) + 4 * (fr & 1));
   }
-  auto compute = [&](int b, Block& x) {
+  // Block b; its registers take over the next block's as soon as they are read.
+  auto compute = [&](int b, bool more) {
     const int k0 = kb.key0(base + b);
-    const int pg[2] = {__builtin_amdgcn_readlane(d0, b), __builtin_amdgcn_readlane(d1, b)};
-    // values into LDS, zeros for those that nobody sees
-    const bool whole = kb.all32(k0) && pg[0] >= 0 && pg[1] >= 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int kk = i * (64 / LPV) + lane / LPV, c = lane % LPV;
-      if (!whole && !(kb.has(k0 + kk) && (kk < 16 ? pg[0] : pg[1]) >= 0)) {
-#pragma unroll
-        for (int w = 0; w < WV; ++w) x.v[i][w] = 0;
-        x.vs[i] = 127;
-      }
-      const float scale = fp4_scale(x.vs[i]);
-#pragma unroll
-      for (int w = 0; w < WV; ++w)
-        *reinterpret_cast<bf16x8*>(vbuf + kk * HD + 8 * wslot<CPK>(kk, c * WV + w)) = fp4_to_bf16(x.v[i][w], scale);
-    }
+    const uint32_t f = __builtin_amdgcn_readlane(flags, b);
     float sv[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -224,45 +272,74 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
       for (int s2 = 0; s2 < KS; ++s2) {
         const bf16x8 k = fp4_to_bf16(x.k[u][s2], scale);
 #pragma unroll
-        for (int i = 0; i < QP; ++i) st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[i][s2], st, 0, 0, 0);
+        for (int i = 0; i < SETS; ++i) st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[i][s2], st, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sv[4 * u + i] = st[i];
+      for (int i = 0; i < 4; ++i) sv[4 * u + i] = parts_sum<SPREAD>(st[i]);
     }
-    // (uniform) some column does not see some key of the block
-    if (k0 + 32 > rs.p0 + 1 || (k0 < lo_last && k0 + 32 > a.sinks) || pg[0] < 0 || pg[1] < 0) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_keys(b + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // values into LDS, zeros for those that nobody sees
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int kk = i * (64 / LPV) + lane / LPV, c = lane % LPV;
+      if (f & PARTLY) {
+        asm volatile("");   // (a branch)
+        if (!kb.has(k0 + kk) || (f & (kk < 16 ? GONE0 : GONE1))) {
+#pragma unroll
+          for (int w = 0; w < WV; ++w) x.v[i][w] = 0;
+          x.vs[i] = 127;
+        }
+      }
+      const float scale = fp4_scale(x.vs[i]);
+      char* dst = reinterpret_cast<char*>(vbuf + kk * HD);
+      const uint32_t first = 16u * wslot<CPK>(kk, c * WV);
+#pragma unroll
+      for (int w = 0; w < WV; ++w) *reinterpret_cast<bf16x8*>(dst + (first ^ (16u * w))) = fp4_to_bf16(x.v[i][w], scale);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_values(b + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (f & EDGE) {   // (uniform)
+      asm volatile("");
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int j = k0 + 4 * fg + (i & 3) + 16 * (i >> 2);
-        const bool sees = j < end_c && (j >= lo_c || j < a.sinks) && pg[i >> 2] >= 0;
+        const bool sees = (j < end_c) & ((j >= lo_c) | (j < a.sinks)) & !(f & (i < 4 ? GONE0 : GONE1));
         if (!sees) sv[i] = -INFINITY;
       }
     }
+    // Probabilities are relative to a maximum up to 2^kStale out of date; the lanes
+    // of a column share it.
     float mt = sv[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mt = fmaxf(mt, sv[i]);
-    mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-    mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-    // rescaled only when some column's maximum grows
-    if (__any(mt > m)) {
+    if (__any(mt > m + kStale)) {
+      mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+      mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
       const float mn = fmaxf(m, mt);
-      const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= corr;
       m = mn;
     }
-    const float mr = m == -INFINITY ? 0.f : m;   // (a column without a key so far)
-    bf16x8 pf[PP];
+    bf16x8 pf[PSETS];
     float ps = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float pv = __builtin_amdgcn_exp2f(sv[i] - mr);
+      float pv = __builtin_amdgcn_exp2f(sv[i] - m);
       ps += pv;
-      __bf16 p[PP];
-      in_parts<PP>(pv, p);
+      if constexpr (F32 && SPREAD > 1) {
+        pf[0][i] = my_part<SPREAD, 3>(pv, part);
+      } else {
+        __bf16 p[PSETS];
+        in_parts<PSETS>(pv, p);
 #pragma unroll
-      for (int j = 0; j < PP; ++j) pf[j][i] = p[j];
+        for (int j = 0; j < PSETS; ++j) pf[j][i] = p[j];
+      }
     }
     l += ps;
     constexpr int N = DT < 4 ? DT : 4;
@@ -270,40 +347,34 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     for (int e0 = 0; e0 < DT; e0 += N) {
       uint32_t va[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) va[i] = vaddr[e0 + i];
+      for (int i = 0; i < N; ++i) va[i] = vaddr ^ (32u * (e0 + i));
       i16x4 lo[N], hi[N];
       lds_read_tr16_pairs<N, 0, 16 * HD * 2>(va, lo, hi);
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < PP; ++j)
+        for (int j = 0; j < PSETS; ++j)
           o[e0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tr16_pair(lo[i], hi[i]), pf[j], o[e0 + i], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // One block ahead.
   while (base < i1) {
     const int nb = imin(64, i1 - base);
-    for (int b = 0; b < nb; b += 2) {
-      if (b + 1 < nb) load_block(b + 1, xb);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(b, xa);
-      if (b + 1 >= nb) break;
-      if (b + 2 < nb) load_block(b + 2, xa);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(b + 1, xb);
-    }
+    for (int b = 0; b < nb; ++b) compute(b, b + 1 < nb);
     base += 64;
-    if (base < i1) {   // (a run of 64 blocks drains: one round trip in 2048 keys)
-      look_up();
-      load_block(0, xa);
-    }
+    if (base < i1) start();   // (a run of 64 blocks drains: one round trip in 2048 keys)
   }
 
   // join the waves: per column the unnormalised output, (max, sum) behind it
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  if constexpr (F32 && SPREAD > 1) {   // the outputs of the probabilities' parts
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dt][e] = parts_sum<SPREAD>(o[dt][e]);
+  }
   __syncthreads();
   float* sm = reinterpret_cast<float*>(lds);   // [NW][16][ROW]
   float* w = sm + (wave * 16 + fr) * ROW;
@@ -394,7 +465,6 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 // barrier a block.  Lane i keeps the place and the mask flags of block i of a
 // run of 64.  The output is rescaled only when a maximum has moved by more than
 // kStale.
-constexpr float kStale = 8.f;
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE, bool F32>
@@ -797,7 +867,7 @@ constexpr int kMaxSplits = 64;
 static int tile_splits(int64_t groups, int64_t blocks) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({kTileTarget / groups, blocks / 8, kMaxSplits}));
 }
-constexpr int kWaveTarget = 2048;
+constexpr int kWaveTarget = 3072;
 constexpr int64_t kShareBytes = 300 << 20;
 
 static Fp4Plan fp4_plan(const PagedAttnArgs& a) {
@@ -815,7 +885,7 @@ static Fp4Plan fp4_plan(const PagedAttnArgs& a) {
     const int64_t pairs = (int64_t)a.rows * a.hkv, blocks = (keys + 31) / 32;
     int64_t want = std::max<int64_t>(1, std::min<int64_t>(kWaveTarget / pairs, blocks / 2));
     if (want > 8 && pairs * 8 >= 1024) want = 8;
-    p.nw = want >= 8 ? 8 : want >= 4 ? 4 : want >= 2 ? 2 : 1;
+    p.nw = want >= 4 ? 4 : want >= 2 ? 2 : 1;
     p.splits = (int)std::min<int64_t>(kMaxSplits, (want + p.nw - 1) / p.nw);
   } else {
     p.tile = true;
@@ -862,16 +932,22 @@ static void launch_fp4(const PagedAttnArgs& a, hipStream_t s) {
       launch_tile<HD, true, F32>(a, common, p.pre, p.slots(), s);
     }
     const dim3 grid(p.splits, a.hkv, a.rows);
-#define SR_FP4_WAVE(NW)                                                                                     \
-  SR_LAUNCH((fp4_wave_kernel<HD, NW, F32>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, \
+    const int cols = a.lr * (a.hq / a.hkv);
+#define SR_FP4_WAVE2(NW, SPREAD)                                                                                    \
+  SR_LAUNCH((fp4_wave_kernel<HD, NW, F32, SPREAD>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, \
             p.pre, p.slots(), qscale)
+#define SR_FP4_WAVE(NW)                                         \
+  do {                                                          \
+    if (cols <= (F32 ? 4 : 8)) SR_FP4_WAVE2(NW, (F32 ? 4 : 2)); \
+    else SR_FP4_WAVE2(NW, 1);                                   \
+  } while (0)
     switch (p.nw) {
-      case 8: SR_FP4_WAVE(8); break;
       case 4: SR_FP4_WAVE(4); break;
       case 2: SR_FP4_WAVE(2); break;
       default: SR_FP4_WAVE(1); break;
     }
 #undef SR_FP4_WAVE
+#undef SR_FP4_WAVE2
     SR_CHECK_LAUNCH();
   }
   if (p.splits > 1) launch_merge<T, HD>(a, p.slots(), s);
