@@ -5,13 +5,21 @@
 // a weight on, and the token is found by an inverse CDF in index order, all on
 // 64-bit integers, so that no grouping of a sum can change a result.
 //
-// A work-group takes a row; its waves take tiles of 1024 entries.  After the
-// maximum, entries are counted (top-k) or weighed (top-p) in bins of z = (l - max)
-// / T, 92 to a unit of z: the bin that holds the border of the kept prefix follows
-// from a scan of the bins.  Where the prefix up to that bin is short enough it is
-// listed in LDS, sorted, cut and drawn from there; else only the border's bin is
-// listed, sorted and cut, and another pass sums the kept weights tile by tile.
+// Few entries matter to most draws, so a row is read twice: for its maximum, and to
+// list its best entries (and weigh all of them where only top-p asks for the
+// total).  Where "best" begins follows from the maxima of 1024 or 2048 subsets of the
+// row: an entry that reaches the k-th largest of them is one of at least k.  Borders
+// are then found in the list by counting and weighing its entries in 2048 bins.  Where
+// the list is not enough (flat rows under top-p, a top-k above 1024, thousands of
+// equals), the whole row goes into bins of z = (l - max) / T, 92 to a unit of z, the
+// border's bin is listed, and another pass sums the kept weights tile by tile.
+//
+//   filtered_kernel         a work-group of 16 waves a row, from the logits to the token
+//   filtered_maxima_kernel, few rows: the two readings by work-groups of four tiles
+//   filtered_list_kernel    each, before filtered_kernel
 #include <algorithm>
+#include <cfloat>
+#include <type_traits>
 
 #include "common.h"
 #include "draw_weights.h"
@@ -26,58 +34,156 @@ constexpr int kFltThreads = 1024;
 constexpr int kFltWaves = kFltThreads / 64;
 constexpr int kFltBins = 2048;     // the last one: entries of weight 0, never counted
 constexpr int kFltList = 4096;     // listed entries
+constexpr int kPLanes = 50;        // lanes of a wave whose maxima the list for top-p starts from
 constexpr int kFltTiles = 256;     // of a row (262144 entries)
+constexpr int kFltSplitWaves = 4;  // tiles of a work-group of the split readings
+constexpr int kFltMaxima = 64 * kFltTiles / kFltSplitWaves;   // of a row, of the split readings
 
-struct FilteredShared {
-  uint64_t mass[kFltBins];   // later: the list's weights, then its draw
+// Work-groups of a row of the split readings.
+__host__ __device__ inline int split_chunks(int vocab) {
+  return (vocab + kFltSplitWaves * kLpTile - 1) / (kFltSplitWaves * kLpTile);
+}
+// A row's scratch of the split readings.
+struct FilteredRow {
+  uint64_t total;            // weight of the row, or of what min-p keeps of it
+  uint32_t n, kept;          // listed; kept by min-p
+  uint64_t tile[kFltTiles];  // weights that min-p keeps, where nothing else filters
   uint64_t list[kFltList];
-  uint64_t tile[kFltTiles];
-  uint64_t wave[kFltWaves + 1];
-  uint32_t count[kFltBins];
-  int n, bin, kept;
-  uint32_t before;
-  uint64_t mass_before;
+  float maxima[kFltMaxima];  // lane l of work-group c: of the entries that it reads
 };
 
-// A row's numbers.
-struct RowDraw {
-  float m, inv_t;
-  bool greedy;
+struct FilteredShared {
+  uint64_t bins[kFltBins];   // counts or weights
+  uint64_t list[kFltList];
+  uint64_t tile[kFltTiles];
+  uint64_t wave[kFltWaves], cand[128];
+  uint64_t before, found, own;
+  uint32_t wave32[kFltWaves];
+  int n, c, bin;
 };
 
 __device__ __forceinline__ float seen(float x) { return fmaxf(x, -INFINITY); }   // NaN counts as -inf
-__device__ __forceinline__ uint64_t row_weight(float l, const RowDraw& r) {
-  return l == r.m ? (uint64_t)1 << 32 : weight_of(l, r.m, r.inv_t);
-}
-// The bin of an entry: monotone in its value.
-__device__ __forceinline__ int row_bin(float l, const RowDraw& r) {
-  const float z = __fmul_rn(__fsub_rn(l, r.m), r.inv_t);
-  const float d = fminf(__fmul_rn(z, -92.f), (float)(kFltBins - 1));   // (z <= -22.25: weight 0)
-  return l == r.m ? 0 : (int)d;
-}
-
-// Inclusive sums over the work-group's threads, and their total.
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* wsum, uint64_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// A row whose maximum is +inf is read as 0 there and -inf elsewhere.
+__device__ __forceinline__ void read_infinite(float (&v)[16]) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t u = shfl_up_u64(v, o);
-    if (lane >= o) v += u;
-  }
-  __syncthreads();
-  if (lane == 63) wsum[wave] = v;
-  __syncthreads();
-  uint64_t base = 0, all = 0;
-  for (int w = 0; w < kFltWaves; ++w) {
-    if (w < wave) base += wsum[w];
-    all += wsum[w];
-  }
-  *total = all;
-  return base + v;
+  for (int e = 0; e < 16; ++e) v[e] = v[e] == INFINITY ? 0.f : -INFINITY;
 }
 
-// Sorts the first n (up to kFltList) words, descending; n2 >= n a power of two.
-__device__ void sort_words(uint64_t* w, int n2) {
+// A row's settings.
+struct RowDraw {
+  float m, inv_t;
+  bool greedy, by_k, by_p;
+  int k;
+  uint32_t least;   // least weight that min-p keeps (2^32 as 2^32 - 1, which no weight is)
+  uint64_t part;
+
+  __device__ __forceinline__ RowDraw(const FilteredArgs& a, int r) {
+    const float t = a.temperature[r], p = a.top_p[r], mp = a.min_p[r];
+    inv_t = (float)(1.0 / (double)t);
+    greedy = !(t > 0.f) || !(inv_t <= 3.402823466e38f);
+    if (greedy) inv_t = 1.f;
+    k = a.top_k[r];
+    by_k = k >= 1 && k < a.vocab;
+    by_p = p < 1.f;   // (false for NaN)
+    part = by_p ? (uint64_t)((double)fmaxf(p, 0.f) * 4294967296.0) : 0;
+    least = mp > 0.f ? (uint32_t)fmin((double)fminf(mp, 1.f) * 4294967296.0, 4294967295.0) : 0;
+  }
+  // A weight, 2^32 as 2^32 - 1; and as it is.
+  __device__ __forceinline__ uint32_t weight_word(float l) const { return weight32(l, m, inv_t); }
+  __device__ __forceinline__ uint64_t weight(float l) const { return weight_of(l, m, inv_t); }
+  // The sum of the weights of 16 entries of which keep(entry, weight word) holds (those
+  // of 2^32, rare beside the maximum's own, are evaluated again; the empty asm keeps
+  // that out of the straight line).
+  template <typename F>
+  __device__ __forceinline__ uint64_t weights(const float (&v)[16], F&& keep) const {
+    uint64_t w = 0;
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t u = weight_word(v[e]);
+      const uint32_t k = keep(e, u) ? u : 0;
+      w += k;
+      top = max(top, k);
+    }
+    if (__builtin_expect(__any(top == 0xFFFFFFFFu), 0)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float l = v[e];
+        asm volatile("" : "+v"(l));
+        const uint32_t u = weight_word(l);
+        w += u == 0xFFFFFFFFu && keep(e, u) ? 1u : 0u;
+      }
+    }
+    return w;
+  }
+  // Where an entry lies among the bins, as a number that grows as values fall.
+  __device__ __forceinline__ float place(float l) const {
+    const float z = __fmul_rn(__fsub_rn(l, m), inv_t);
+    return fminf(__fmul_rn(z, -92.f), (float)(kFltBins - 1));   // (z <= -22.25: weight 0)
+  }
+  __device__ __forceinline__ int bin(float l) const { return (int)place(l); }
+  // The least weight of a prefix that holds top_p of `total`.
+  __device__ __forceinline__ uint64_t needed(uint64_t total) const {
+    const uint64_t low = part * (total & 0xFFFFFFFFull);
+    const uint64_t need = part * (total >> 32) + (low >> 32) + ((low & 0xFFFFFFFFull) ? 1 : 0);
+    return need > 1 ? need : (uint64_t)1;
+  }
+};
+
+__device__ __forceinline__ uint64_t scaled_word(uint64_t x, uint64_t total) {   // floor(x total / 2^32)
+  return x * (total >> 32) + ((x * (total & 0xFFFFFFFFull)) >> 32);
+}
+
+// Inclusive sums over the lanes, by DPP: within rows of 16, then from row to row.
+template <typename F>
+__device__ __forceinline__ void wave_scan_steps(F&& step) {
+  step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xF>{});   // row_shr 1, 2, 4, 8
+  step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xF>{});
+  step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xF>{});
+  step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xF>{});
+  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast 15, 31
+  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
+}
+__device__ __forceinline__ uint32_t wave_scan32(uint32_t v) {
+  wave_scan_steps([&](auto ctrl, auto rows) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  });
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {
+  wave_scan_steps([&](auto ctrl, auto rows) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    v += (uint64_t)hi << 32 | lo;
+  });
+  return v;
+}
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// The sum over the threads up to this one, and of all.
+struct Scan {
+  uint64_t upto, all;
+};
+__device__ __forceinline__ Scan block_scan(uint64_t v, FilteredShared& sh) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  v = wave_scan64(v);
+  __syncthreads();   // (the last scan's sums are read)
+  if (lane == 63) sh.wave[wave] = v;
+  __syncthreads();
+  const uint64_t w = wave_scan64(lane < kFltWaves ? sh.wave[lane] : 0);
+  return {v + (wave > 0 ? lane_value(w, wave - 1) : 0), lane_value(w, 63)};
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  wave_scan_steps([&](auto ctrl, auto rows) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+  });
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Sorts n2 (a power of two) words of the list, descending.
+__device__ __forceinline__ void sort_words(uint64_t* w, int n2) {
   for (int k = 2; k <= n2; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
       for (int i = threadIdx.x; i < n2 / 2; i += kFltThreads) {
@@ -92,21 +198,154 @@ __device__ void sort_words(uint64_t* w, int n2) {
     }
 }
 
-__device__ __forceinline__ uint64_t scaled_word(uint64_t x, uint64_t total) {   // floor(x total / 2^32)
-  return x * (total >> 32) + ((x * (total & 0xFFFFFFFFull)) >> 32);
+__device__ __forceinline__ void clear_bins(FilteredShared& sh) {
+  for (int i = threadIdx.x; i < kFltBins; i += kFltThreads) sh.bins[i] = 0;
+  if (threadIdx.x == 0) sh.c = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void add_to_bin(FilteredShared& sh, int b, uint64_t v) {
+  atomicAdd((unsigned long long*)&sh.bins[b], (unsigned long long)v);
+}
+// The bins' sums over threads of two bins each.
+__device__ __forceinline__ Scan scan_bins(FilteredShared& sh) {
+  __syncthreads();
+  return block_scan(sh.bins[2 * threadIdx.x] + sh.bins[2 * threadIdx.x + 1], sh);
+}
+// The first bin up to which they reach `target`, which they do: sh.bin, and what lies
+// before it in sh.before.
+__device__ __forceinline__ void find_bin(FilteredShared& sh, const Scan& s, uint64_t target) {
+  const int i = 2 * threadIdx.x;
+  const uint64_t exc = s.upto - sh.bins[i] - sh.bins[i + 1], mid = exc + sh.bins[i];
+  if (exc < target && target <= s.upto) {
+    sh.bin = mid < target ? i + 1 : i;
+    sh.before = mid < target ? mid : exc;
+  }
+  __syncthreads();
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kFltThreads) filtered_kernel(FilteredArgs a) {
+// Borders and draws from a list of n entries: by top-k, by top-p, by index.  Each is
+// the same search: entries of some size in 2048 bins, the bin that holds the sought
+// point, and the entry among those of the bin.
+struct ListCut {
+  uint64_t border;      // words below it are not kept
+  uint64_t found;       // the last search's entry (0: the list does not reach the point)
+  uint64_t all, own;    // the last search's sum, and the found entry's part of it
+  uint32_t kept;        // entries of it
+};
+enum { BY_K = 1, BY_P = 2, BY_INDEX = 4 };
+// rank_k: the entries to keep; total: the weight that top-p goes by (0: of what is kept);
+// rank_p: instead of it where not 0; bins over places [lo, lo + kFltBins / scale); least:
+// the value that top-k's border has to reach (else nothing is found).
+__device__ __forceinline__ ListCut cut_list(FilteredShared& sh, const RowDraw& rd, int n, int searches, uint64_t rank_k,
+                                            uint64_t total, uint64_t rank_p, float lo, float scale, uint64_t word,
+                                            float least = -FLT_MAX) {
+  ListCut r{0, 0, 0, 0, 0};
+  for (int which = BY_K; which <= BY_INDEX; which <<= 1) {   // (uniform; one body for the three)
+    if (!(searches & which)) continue;
+    clear_bins(sh);
+    auto bin_of = [&](uint64_t w) {
+      if (which == BY_INDEX) return word_index(w) >> 7;
+      return min(kFltBins - 1, max(0, (int)((rd.place(word_value(w)) - lo) * scale)));
+    };
+    auto size_of = [&](uint64_t w) -> uint64_t {
+      if (w < r.border) return 0;
+      if (which == BY_K) return 1;
+      const uint32_t u = rd.weight_word(word_value(w));
+      if (which == BY_INDEX && u < rd.least) return 0;
+      return (uint64_t)u + (u == 0xFFFFFFFFu ? 1 : 0);
+    };
+    uint32_t kept = 0;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kFltThreads) {
+      const uint64_t w = sh.list[i], u = size_of(w);
+      if (u == 0) continue;
+      ++kept;
+      add_to_bin(sh, bin_of(w), u);
+    }
+    kept = wave_scan32(kept);   // (of the wave, in its last lane)
+    if ((threadIdx.x & 63) == 63) sh.wave32[threadIdx.x >> 6] = kept;
+    const Scan s = scan_bins(sh);
+    r.all = s.all;
+    r.kept = __builtin_amdgcn_readlane(wave_scan32((threadIdx.x & 63) < kFltWaves ? sh.wave32[threadIdx.x & 63] : 0), 63);
+    uint64_t rank = which == BY_K ? rank_k : which == BY_INDEX ? scaled_word(word, s.all) + 1
+                                                               : rank_p ? rank_p : rd.needed(total ? total : s.all);
+    if (s.all < rank) {   // (uniform)
+      r.found = 0;
+      return r;
+    }
+    find_bin(sh, s, rank);
+    const int bin = sh.bin;
+    rank -= sh.before;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kFltThreads) {
+      const uint64_t w = sh.list[i];
+      if (bin_of(w) != bin || size_of(w) == 0) continue;
+      const int at = atomicAdd(&sh.c, 1);
+      if (at < 128) sh.cand[at] = w;
+    }
+    __syncthreads();
+    const int c = sh.c;
+    if (c <= 128) {   // (always, by index)
+      if ((int)threadIdx.x < c) {
+        // larger words first; by index: larger inverted indices
+        const uint64_t mask = which == BY_INDEX ? 0xFFFFFFFFull : ~0ull;
+        const uint64_t mine = sh.cand[threadIdx.x], own = size_of(mine);
+        uint64_t before = 0;
+#pragma unroll 1
+        for (int j = 0; j < c; ++j) {
+          const uint64_t w = sh.cand[j];
+          if ((w & mask) > (mine & mask)) before += size_of(w);
+        }
+        if (before < rank && rank <= before + own) {
+          sh.found = mine;
+          sh.own = own;
+        }
+      }
+      __syncthreads();
+    } else {   // many alike: in order
+      int n2 = 1;
+      while (n2 < n) n2 <<= 1;
+      for (int i = n + threadIdx.x; i < n2; i += kFltThreads) sh.list[i] = 0;
+      __syncthreads();
+      sort_words(sh.list, n2);
+      uint64_t sum = 0;
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {   // (the bin's entries lie together)
+        const int i = 4 * threadIdx.x + e;
+        if (i < n && bin_of(sh.list[i]) == bin) sum += size_of(sh.list[i]);
+      }
+      uint64_t run = block_scan(sum, sh).upto - sum;
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * threadIdx.x + e;
+        const uint64_t u = i < n && bin_of(sh.list[i]) == bin ? size_of(sh.list[i]) : 0;
+        if (run < rank && rank <= run + u) sh.found = sh.list[i];
+        run += u;
+      }
+      __syncthreads();
+    }
+    r.found = sh.found;
+    r.own = sh.own;
+    if (which != BY_INDEX) r.border = r.found;
+    if (which == BY_K && word_value(r.border) < least) {   // (uniform)
+      r.found = 0;
+      return r;
+    }
+  }
+  return r;
+}
+
+// SPLIT: the row's maxima and list come from the split readings.
+template <typename T, bool VEC, bool SPLIT>
+__global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a) {
   __shared__ FilteredShared sh;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* x = (const T*)a.logits + r * a.row_stride;
   const int vocab = a.vocab;
-  const float T_ = a.temperature[r];
-  RowDraw rd;
-  rd.inv_t = (float)(1.0 / (double)T_);
-  rd.greedy = !(T_ > 0.f) || !(rd.inv_t <= 3.402823466e38f);
+  RowDraw rd(a, r);
+  const FilteredRow* given = SPLIT ? (const FilteredRow*)a.scratch + r : nullptr;
+  bool infinite = false;
 
   // f(values, base) for the wave's tiles, the next one's loads in flight
   auto pass = [&](auto&& f) {
@@ -116,382 +355,514 @@ __global__ void __launch_bounds__(kFltThreads) filtered_kernel(FilteredArgs a) {
     if (base < vocab) Tile<T, VEC>::load(x, base, vocab, lane, v);
     for (; base < vocab; base += step) {
       if (base + step < vocab) Tile<T, VEC>::load(x, base + step, vocab, lane, nx);
+      if (infinite) read_infinite(v);
       f(v, base);
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] = nx[e];
     }
   };
+  auto entry_at = [&](int i) {
+    const float l = seen(to_f32<T>(x[i]));
+    return !infinite ? l : l == INFINITY ? 0.f : -INFINITY;
+  };
   auto index = [&](int base, int e) { return Tile<T, VEC>::index(base, e, lane); };
-
-  // the best entry
-  uint64_t best = 0;
-  {
-    float mt = -INFINITY;
-    int at = 0;
-    pass([&](const float(&v)[16], int base) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (v[e] > mt) {
-          mt = v[e];
-          at = index(base, e);
-        }
-    });
-    best = entry_word(mt, at);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t u = shfl_xor_u64(best, o);
-      best = u > best ? u : best;
-    }
-    if (lane == 0) sh.wave[wave] = best;
-    __syncthreads();
-    for (int w = 0; w < kFltWaves; ++w) best = sh.wave[w] > best ? sh.wave[w] : best;
-    __syncthreads();
-  }
-  rd.m = word_value(best);
   auto answer = [&](int token, float lp, int kept) {   // (one thread)
     if (a.token) a.token[r] = token;
     if (a.logprob) a.logprob[r] = lp;
     if (a.kept) a.kept[r] = kept;
   };
+
+  // Lists those of a tile that reach `from`: one reservation a wave, its lanes' entries
+  // one lane after the other.
+  auto list_from = [&](const float(&v)[16], int base, float from) {
+    uint32_t in = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) in |= (uint32_t)(v[e] >= from) << e;
+    if (!__any(in != 0)) return;
+    const uint32_t mine = __popc(in), upto = wave_scan32(mine);
+    int at = 0;
+    if (lane == 63) at = atomicAdd(&sh.n, (int)upto);
+    at = __builtin_amdgcn_readlane(at, 63) + (int)(upto - mine);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (in >> e & 1) {
+        if (at < kFltList) sh.list[at] = entry_word(v[e], index(base, e));
+        ++at;
+      }
+  };
+  // A key that `want` of the wave's lanes reach with theirs (its upper 16 bits).
+  auto reached = [&](uint32_t key, int want) {
+    uint32_t t = 0;
+#pragma unroll 1
+    for (int b = 31; b >= 16; --b) {
+      const uint32_t c = t | (1u << b);
+      if (__popcll(__ballot(key >= c)) >= want) t = c;
+    }
+    return t;
+  };
+  auto key_of = [&](float l) { return (uint32_t)(entry_word(seen(l), 0) >> 32); };
+  // (bits below -inf's read as a NaN)
+  auto value_of = [&](uint32_t key) {
+    const float f = word_value((uint64_t)key << 32);
+    return f > -FLT_MAX ? f : -FLT_MAX;
+  };
+
+  // The maximum.  Under a top-k of a long row, every wave also lists what reaches a bound
+  // that it takes from its first tile: if the k-th of the listed reaches the highest of
+  // these bounds, the list holds the first k.  Else a value that at least k entries
+  // reach is the least of the waves' k / waves-th largest lanes' maxima (of those that have
+  // a whole tile), and another pass lists them.
+  const int whole = min(kFltWaves, vocab / kLpTile);
+  const bool by_list = (rd.by_k && (rd.k <= 64 * whole || vocab <= kFltList)) || (!rd.by_k && rd.by_p);
+  const bool at_once = !SPLIT && rd.by_k && !rd.greedy && rd.k <= kFltThreads && vocab >= 2 * kFltWaves * kLpTile;
+  float from = -FLT_MAX, highest = -FLT_MAX;
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  {
+    float mt = -INFINITY;
+    uint32_t bound = ~0u, first = 0;
+    if constexpr (SPLIT) {
+      for (int i = tid; i < split_chunks(vocab) * 64; i += kFltThreads) mt = fmaxf(mt, given->maxima[i]);
+    } else {
+      float own = INFINITY;
+      pass([&](const float(&v)[16], int base) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mt = fmaxf(mt, v[e]);
+        if (at_once) {
+          if (base == wave * kLpTile) {
+            first = reached(key_of(mt), min(64, 8 + (int)(2 * (int64_t)rd.k * kLpTile / vocab)));
+            own = value_of(first);
+          }
+          list_from(v, base, own);
+        }
+      });
+      if (wave < whole) bound = reached(key_of(mt), rd.by_k ? (rd.k + whole - 1) / whole : kPLanes);
+    }
+    const uint32_t best = wave_max_u32(key_of(mt));
+    if (lane == 0) {
+      sh.wave[wave] = (uint64_t)best << 32 | (uint32_t)~bound;
+      sh.wave32[wave] = first;
+    }
+    __syncthreads();
+    const uint64_t w = lane < kFltWaves ? sh.wave[lane] : 0;
+    rd.m = word_value((uint64_t)wave_max_u32((uint32_t)(w >> 32)) << 32);
+    if (vocab > kFltList) from = value_of(~wave_max_u32((uint32_t)w));
+    highest = value_of(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0));
+  }
   if (rd.m == -INFINITY) {
     if (tid == 0) answer(0, -INFINITY, 0);
     return;
   }
+  if (rd.m == INFINITY) {
+    infinite = true;
+    rd.m = 0.f;
+    from = from == INFINITY ? 0.f : -FLT_MAX;
+  }
   if (rd.greedy) {
-    if (tid == 0) answer(word_index(best), 0.f, 1);
+    int at = 0x7FFFFFFF;
+    if (SPLIT && given->n <= kFltList) {
+      for (int i = tid; i < (int)given->n; i += kFltThreads)
+        if (word_value(given->list[i]) == rd.m) at = min(at, word_index(given->list[i]));
+    } else {
+      pass([&](const float(&v)[16], int base) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (v[e] == rd.m) at = min(at, index(base, e));
+      });
+    }
+    __syncthreads();
+    const uint32_t best = wave_max_u32(~(uint32_t)at);
+    if (lane == 0) sh.wave32[wave] = best;
+    __syncthreads();
+    const uint32_t all = wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0);
+    if (tid == 0) answer((int)~all, 0.f, 1);
     return;
   }
   const uint64_t word = a.random[r * a.random_stride];
-  const int top_k = a.top_k[r];
-  const float top_p = a.top_p[r], min_p = a.min_p[r];
-  const bool by_p = top_p < 1.f;   // (false for NaN)
-  const uint64_t part = by_p ? (uint64_t)((double)fmaxf(top_p, 0.f) * 4294967296.0) : 0;
-  const uint64_t least = min_p > 0.f ? (uint64_t)((double)fminf(min_p, 1.f) * 4294967296.0) : 0;
-  // the least weight of a prefix that holds top_p of `total`
-  auto needed = [&](uint64_t total) {
-    const uint64_t low = part * (total & 0xFFFFFFFFull);
-    const uint64_t need = part * (total >> 32) + (low >> 32) + ((low & 0xFFFFFFFFull) ? 1 : 0);
-    return need > 1 ? need : (uint64_t)1;
+  auto draw = [&](const ListCut& c) {
+    if (tid == 0) answer(word_index(c.found), (float)log((double)c.own / (double)c.all), (int)c.kept);
   };
-  uint64_t border = 0;   // words below it are not kept
 
-  // Fills the bins with counts (and weights) of the entries from `border` on.
-  auto fill = [&](bool weigh) {
-    for (int i = tid; i < kFltBins; i += kFltThreads) {
-      sh.count[i] = 0;
-      if (weigh) sh.mass[i] = 0;
-    }
-    __syncthreads();
-    pass([&](const float(&v)[16], int base) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float l = seen(v[e]);
-        const int b = row_bin(l, rd);
-        if (b < kFltBins - 1 && entry_word(l, index(base, e)) >= border) {
-          atomicAdd(&sh.count[b], 1u);
-          if (weigh) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)row_weight(l, rd));
+  // The list of the best, where it can be enough.
+  if (by_list) {
+    int n;
+    uint64_t total = 0;
+    float end = 0.f;
+    if constexpr (SPLIT) {
+      n = (int)given->n;
+      total = given->total;
+      if (n <= kFltList)
+        for (int i = tid; i < n; i += kFltThreads) {
+          sh.list[i] = given->list[i];
+          end = fmaxf(end, rd.place(word_value(sh.list[i])));
         }
+    } else if (at_once && !infinite) {
+      n = sh.n;
+      end = (float)(kFltBins - 1);
+    } else {
+      const bool weigh = !rd.by_k;
+      end = rd.place(from);
+      __syncthreads();
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      pass([&](const float(&v)[16], int base) {
+        if (weigh) total += rd.weights(v, [](int, uint32_t) { return true; });
+        list_from(v, base, from);
+      });
+      total = block_scan(total, sh).all;   // (and every entry is listed)
+      n = sh.n;
+    }
+    if constexpr (SPLIT) {
+      // (places are not negative: their bits order them)
+      const uint32_t best = wave_max_u32(__float_as_uint(end));
+      if (lane == 0) sh.wave32[wave] = best;
+      __syncthreads();
+      end = __uint_as_float(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0));
+      __syncthreads();
+    }
+    if (n <= kFltList && (!at_once || infinite || n >= rd.k)) {
+      const int searches = (rd.by_k && (at_once || n > rd.k) ? BY_K : 0) | (rd.by_p ? BY_P : 0) | BY_INDEX;
+      const ListCut c = cut_list(sh, rd, n, searches, (uint64_t)rd.k, rd.by_k ? 0 : total, 0, 0.f,
+                                 (float)kFltBins / (end + 1.f), word, at_once && !infinite ? highest : -FLT_MAX);
+      if (c.found) {
+        draw(c);
+        return;
       }
-    });
-    __syncthreads();
-  };
-  // The first bin up to which the counts (or weights) reach `target`, with what
-  // lies before it; false where all together do not.
-  auto find = [&](bool weigh, uint64_t target, uint64_t* total) {
-    const int i = 2 * tid;
-    const uint64_t v0 = weigh ? sh.mass[i] : sh.count[i], v1 = weigh ? sh.mass[i + 1] : sh.count[i + 1];
-    const uint64_t inc = block_scan(v0 + v1, sh.wave, total), exc = inc - v0 - v1;
-    if (exc < target && target <= inc) sh.bin = exc + v0 >= target ? i : i + 1;
-    __syncthreads();
-    if (*total < target) return false;
-    // what lies before: counts and weights alike
-    uint64_t all;
-    const int b = sh.bin;
-    const uint64_t ci = block_scan((i < b ? sh.count[i] : 0) + (i + 1 < b ? sh.count[i + 1] : 0), sh.wave, &all);
-    (void)ci;
-    if (tid == 0) sh.before = (uint32_t)all;
-    if (weigh) {
-      block_scan((i < b ? sh.mass[i] : 0) + (i + 1 < b ? sh.mass[i + 1] : 0), sh.wave, &all);
-      if (tid == 0) sh.mass_before = all;
     }
     __syncthreads();
-    return true;
-  };
-  // Lists the entries for which f holds (at most kFltList, as the caller knows),
-  // sorted; returns their number.
-  auto listed = [&](auto&& f) {
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    pass([&](const float(&v)[16], int base) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float l = seen(v[e]);
-        const uint64_t w = entry_word(l, index(base, e));
-        const bool in = index(base, e) < vocab && f(l, w);
-        const uint64_t mask = __ballot(in);
-        if (mask == 0) continue;
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&sh.n, __popcll(mask));
-        at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
-        if (in && at < kFltList) sh.list[at] = w;
-      }
-    });
-    __syncthreads();
-    const int n = min(sh.n, kFltList);
-    int n2 = 1;
-    while (n2 < n) n2 <<= 1;
-    for (int i = n + tid; i < n2; i += kFltThreads) sh.list[i] = 0;
-    __syncthreads();
-    sort_words(sh.list, n2);
-    return n;
-  };
-  // The `rank`-th entry in order (from 1, by counts) or the first one up to which
-  // the weights reach `rank`, among the entries of bin `b`: refined by digits of
-  // their values until a list holds them, and by index among equals.
-  auto border_in = [&](int b, uint64_t rank, bool weigh) -> uint64_t {
-    uint32_t prefix = 0;   // upper bits of the values' keys that are settled
-    int bits = 0;
-    int n = (int)sh.count[b];
-    __syncthreads();
-    auto in_prefix = [&](uint64_t w) { return bits == 0 || (uint32_t)(w >> 32) >> (32 - bits) == prefix; };
-    while (n > kFltList && bits < 32) {
+  }
+
+  // The whole row: top-k's border, then top-p's among what that keeps.
+  uint64_t border = 0;   // words below it are not kept
+  for (int which = BY_K; which <= BY_P; which <<= 1) {   // (uniform)
+    const bool by_mass = which == BY_P;
+    if (by_mass ? !rd.by_p : !rd.by_k) continue;
+    // entries of bin `b` (any bin: -1) and of the values whose upper `bits` are `prefix`
+    int b = -1, bits = 0;
+    uint32_t prefix = 0;
+    uint64_t rank = 0;
+    auto asked = [&](float l, uint64_t w) {
+      return w >= border && (b < 0 ? rd.bin(l) < kFltBins - 1 : rd.bin(l) == b) &&
+             (bits == 0 || (uint32_t)(w >> 32) >> (32 - bits) == prefix);
+    };
+    bool some = true;
+    uint64_t found = 0;
+    while (true) {   // by bins, then by digits of the values (the largest first), until a list holds them
       const int digit = min(11, 32 - bits);
-      for (int i = tid; i < kFltBins; i += kFltThreads) {
-        sh.count[i] = 0;
-        sh.mass[i] = 0;
-      }
-      __syncthreads();
+      clear_bins(sh);
       pass([&](const float(&v)[16], int base) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float l = seen(v[e]);
           const uint64_t w = entry_word(l, index(base, e));
-          if (row_bin(l, rd) == b && w >= border && in_prefix(w)) {
-            // (descending: the largest digit first)
-            const int d = (1 << digit) - 1 - (int)(((uint32_t)(w >> 32) >> (32 - bits - digit)) & ((1u << digit) - 1));
-            atomicAdd(&sh.count[d], 1u);
-            if (weigh) atomicAdd((unsigned long long*)&sh.mass[d], (unsigned long long)row_weight(l, rd));
-          }
+          if (!asked(l, w)) continue;
+          const int to = b < 0 ? rd.bin(l)
+                               : (1 << digit) - 1 - (int)(((uint32_t)(w >> 32) >> (32 - bits - digit)) & ((1u << digit) - 1));
+          add_to_bin(sh, to, by_mass ? rd.weight(l) : 1);
+        }
+      });
+      const Scan s = scan_bins(sh);
+      if (b < 0) {
+        rank = by_mass ? rd.needed(s.all) : (uint64_t)rd.k;
+        some = s.all >= rank;
+        if (!some) break;   // (fewer than top_k have weights)
+      }
+      find_bin(sh, s, rank);
+      rank -= sh.before;
+      if (b < 0) {
+        b = sh.bin;
+      } else {
+        prefix = (prefix << digit) | (uint32_t)((1 << digit) - 1 - sh.bin);
+        bits += digit;
+      }
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      pass([&](const float(&v)[16], int base) {
+        uint32_t in = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float l = seen(v[e]);
+          in |= (uint32_t)asked(l, entry_word(l, index(base, e))) << e;
+        }
+#pragma unroll 1
+        while (in) {
+          const int e = __builtin_ctz(in), at = atomicAdd(&sh.n, 1);
+          in &= in - 1;
+          float l = v[0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) l = e == i ? v[i] : l;
+          if (at < kFltList) sh.list[at] = entry_word(seen(l), index(base, e));
         }
       });
       __syncthreads();
-      uint64_t total;
-      find(weigh, rank, &total);
-      rank -= weigh ? sh.mass_before : sh.before;
-      n = (int)sh.count[sh.bin];
-      prefix = (prefix << digit) | (uint32_t)((1 << digit) - 1 - sh.bin);
-      bits += digit;
+      const int n = sh.n;
+      if (n <= kFltList) {
+        found = cut_list(sh, rd, n, which, rank, 0, rank, (float)b, (float)kFltBins, word).found;
+        break;
+      }
+      if (bits == 32) break;
       __syncthreads();
     }
-    if (n <= kFltList) {
-      n = listed([&](float l, uint64_t w) { return row_bin(l, rd) == b && w >= border && in_prefix(w); });
-      // four entries a thread
-      uint64_t w4[4], sum = 0, total;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 4 * tid + e;
-        w4[e] = i >= n ? 0 : weigh ? row_weight(word_value(sh.list[i]), rd) : 1;
-        sum += w4[e];
+    if (!some) continue;
+    if (found == 0) {
+      // all equal: by index, of their common weight (at least 1: bin b is counted)
+      if (by_mass) {
+        const uint64_t w = rd.weight(word_value((uint64_t)prefix << 32));
+        rank = (rank + w - 1) / w;
       }
-      uint64_t run = block_scan(sum, sh.wave, &total) - sum;
+      if (tid < kFltTiles) sh.tile[tid] = 0;
+      __syncthreads();
+      auto tied = [&](float l, int i) {
+        const uint64_t w = entry_word(l, i);
+        return (uint32_t)(w >> 32) == prefix && w >= border;
+      };
+      pass([&](const float(&v)[16], int base) {
+        int c = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (run < rank && rank <= run + w4[e]) sh.bin = 4 * tid + e;
-        run += w4[e];
+        for (int e = 0; e < 16; ++e) c += __popcll(__ballot(tied(seen(v[e]), index(base, e))));
+        if (lane == 0) sh.tile[base / kLpTile] = (uint64_t)c;
+      });
+      __syncthreads();
+      const uint64_t mine = tid < kFltTiles ? sh.tile[tid] : 0;
+      uint64_t upto = block_scan(mine, sh).upto;
+      if (upto - mine < rank && rank <= upto) {
+        sh.bin = tid;
+        sh.before = upto - mine;
       }
       __syncthreads();
-      const uint64_t found = sh.list[sh.bin];
+      rank -= sh.before;
+      const int i = sh.bin * kLpTile + tid;   // an entry a thread
+      const bool in = i < vocab && tied(entry_at(min(i, vocab - 1)), i);
+      upto = block_scan(in ? 1 : 0, sh).upto;
+      if (in && upto == rank) sh.bin = i;
       __syncthreads();
-      return found;
-    }
-    // all equal: by index, of their common weight (at least 1: bin b is counted)
-    const float l = word_value((uint64_t)prefix << 32);
-    if (weigh) {
-      const uint64_t w = row_weight(l, rd);
-      rank = (rank + w - 1) / w;
-    }
-    if (tid < kFltTiles) sh.tile[tid] = 0;
-    __syncthreads();
-    auto tied = [&](float v, int i) {
-      const uint64_t w = entry_word(seen(v), i);
-      return i < vocab && (uint32_t)(w >> 32) == prefix && w >= border;
-    };
-    pass([&](const float(&v)[16], int base) {
-      int c = 0;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) c += __popcll(__ballot(tied(v[e], index(base, e))));
-      if (lane == 0) sh.tile[base / kLpTile] = (uint64_t)c;
-    });
-    uint64_t total;
-    __syncthreads();
-    const uint64_t mine = tid < kFltTiles ? sh.tile[tid] : 0;
-    uint64_t inc = block_scan(mine, sh.wave, &total);
-    if (inc - mine < rank && rank <= inc) {
-      sh.bin = tid;
-      sh.mass_before = inc - mine;
-    }
-    __syncthreads();
-    rank -= sh.mass_before;
-    const int i = sh.bin * kLpTile + tid;   // an entry a thread
-    const bool in = i < vocab && tied(to_f32<T>(x[min(i, vocab - 1)]), i);
-    inc = block_scan(in ? 1 : 0, sh.wave, &total);
-    if (in && inc == rank) sh.bin = i;
-    __syncthreads();
-    const uint64_t found = ((uint64_t)prefix << 32) | (uint32_t)~sh.bin;
-    __syncthreads();
-    return found;
-  };
-
-  // What the list of the leading bins holds, cut by the filters and drawn from.
-  auto draw_from_list = [&](int last_bin, uint64_t keep, bool p_total_known, uint64_t p_total) {
-    const int n = listed([&](float l, uint64_t) { return row_bin(l, rd) <= last_bin; });
-    const int cut = (int)(keep < (uint64_t)n ? keep : (uint64_t)n);
-    uint64_t w4[4], sum = 0, total;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * tid + e;
-      w4[e] = i < cut ? row_weight(word_value(sh.list[i]), rd) : 0;
-      sum += w4[e];
-    }
-    uint64_t run = block_scan(sum, sh.wave, &total) - sum;
-    if (by_p) {
-      const uint64_t need = needed(p_total_known ? p_total : total);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint64_t w = w4[e];
-        if (run >= need) w4[e] = 0;
-        run += w;
-      }
-    }
-    int kept = 0, n_pow = 1;
-    sum = 0;
-    while (n_pow < n) n_pow <<= 1;
-    __syncthreads();
-    // by index: words of (inverted index, weight), descending
-    uint64_t i4[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * tid + e;
-      if (w4[e] < least) w4[e] = 0;
-      kept += w4[e] != 0;
-      sum += w4[e];
-      i4[e] = i < n ? ((uint64_t)(0x3FFFF - word_index(sh.list[i])) << 33) | w4[e] : 0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (4 * tid + e < n_pow) sh.list[4 * tid + e] = i4[e];
-    block_scan((uint64_t)kept, sh.wave, &total);
-    kept = (int)total;
-    block_scan(sum, sh.wave, &total);
-    sort_words(sh.list, n_pow);
-    const uint64_t t = scaled_word(word, total);
-    sum = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      i4[e] = 4 * tid + e < n ? sh.list[4 * tid + e] : 0;
-      sum += i4[e] & 0x1FFFFFFFFull;
-    }
-    uint64_t all;
-    run = block_scan(sum, sh.wave, &all) - sum;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint64_t w = i4[e] & 0x1FFFFFFFFull;
-      if (run <= t && t < run + w)
-        answer(0x3FFFF - (int)(i4[e] >> 33), (float)log((double)w / (double)total), kept);
-      run += w;
-    }
-  };
-
-  if (top_k >= 1 && top_k < vocab) {
-    fill(false);
-    uint64_t total;
-    if (find(false, (uint64_t)top_k, &total)) {
-      const int b = sh.bin;
-      if (sh.before + sh.count[b] <= kFltList) {
-        __syncthreads();
-        draw_from_list(b, (uint64_t)top_k, false, 0);
-        return;
-      }
-      const uint64_t rank = (uint64_t)top_k - sh.before;
-      border = border_in(b, rank, false);
-    }
-  }
-  if (by_p) {
-    fill(true);
-    uint64_t total;
-    find(true, ~0ull, &total);
-    const uint64_t need = needed(total);
-    find(true, need, &total);
-    const int b = sh.bin;
-    if (border == 0 && sh.before + sh.count[b] <= kFltList) {
+      found = ((uint64_t)prefix << 32) | (uint32_t)~sh.bin;
       __syncthreads();
-      draw_from_list(b, ~0ull, true, total);
-      return;
     }
-    const uint64_t rank = need - sh.mass_before;
-    border = border_in(b, rank, true);
+    border = found;
   }
 
-  // the kept weights tile by tile, then the tile, run and entry of the drawn point
-  auto kept_weight = [&](float v, int i) -> uint64_t {
-    const float l = seen(v);
-    if (!(l > -INFINITY) || entry_word(l, i) < border) return 0;
-    const uint64_t w = row_weight(l, rd);
-    return w >= least ? w : 0;
+  // the kept weights tile by tile, then the tile and entry of the drawn point
+  const float value = border ? word_value(border) : -FLT_MAX;   // the border's, or the lowest
+  const int at_most = border ? word_index(border) : 0x7FFFFFFF;
+  auto is_kept = [&](float l, int i, uint32_t u) {
+    return ((l > value) | ((l == value) & (i <= at_most))) & (u >= rd.least);
   };
+  uint64_t kept = 0;
   if (tid < kFltTiles) sh.tile[tid] = 0;
-  int kept = 0;
   __syncthreads();
-  pass([&](const float(&v)[16], int base) {
-    uint64_t w = 0;
+  if (SPLIT && !rd.by_k && !rd.by_p) {
+    if (tid < (vocab + kLpTile - 1) / kLpTile) sh.tile[tid] = given->tile[tid];
+    kept = tid == 0 ? given->kept : 0;
+  } else {
+    pass([&](const float(&v)[16], int base) {
+      float top = v[0];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const uint64_t u = kept_weight(v[e], index(base, e));
-      w += u;
-      kept += u != 0;
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) w += shfl_xor_u64(w, o);
-    if (lane == 0) sh.tile[base / kLpTile] = w;
-  });
-  uint64_t total;
-  block_scan((uint64_t)kept, sh.wave, &total);
-  kept = (int)total;
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, v[e]);
+      if (!__any(top >= value)) return;
+      uint32_t mine = 0;
+      uint64_t w = rd.weights(v, [&](int e, uint32_t u) {
+        const bool in = is_kept(v[e], index(base, e), u);
+        mine |= (uint32_t)(in && u != 0) << e;
+        return in;
+      });
+      kept += __popc(mine);
+      w = wave_scan64(w);
+      if (lane == 63) sh.tile[base / kLpTile] = w;
+    });
+  }
+  kept = block_scan(kept, sh).all;   // (and the tiles are written)
   const uint64_t mine = tid < kFltTiles ? sh.tile[tid] : 0;
-  uint64_t inc = block_scan(mine, sh.wave, &total);
-  uint64_t t = scaled_word(word, total);
-  if (inc - mine <= t && t < inc) {
+  const Scan s = block_scan(mine, sh);
+  uint64_t t = scaled_word(word, s.all);
+  if (s.upto - mine <= t && t < s.upto) {
     sh.bin = tid;
-    sh.mass_before = inc - mine;
+    sh.before = s.upto - mine;
   }
   __syncthreads();
-  t -= sh.mass_before;
+  t -= sh.before;
   const int i = sh.bin * kLpTile + tid;   // an entry a thread
-  const uint64_t w = i < vocab ? kept_weight(to_f32<T>(x[i]), i) : 0;
-  uint64_t all;
-  inc = block_scan(w, sh.wave, &all);
-  if (inc - w <= t && t < inc) answer(i, (float)log((double)w / (double)total), kept);
+  uint64_t w = 0;
+  if (i < vocab) {
+    const float l = entry_at(i);
+    w = is_kept(l, i, rd.weight_word(l)) ? rd.weight(l) : 0;
+  }
+  const uint64_t upto = block_scan(w, sh).upto;
+  if (upto - w <= t && t < upto) answer(i, (float)log((double)w / (double)s.all), (int)kept);
 }
 
+// ------------------------------------------------------------- split readings
+// Work-group = (four tiles of a row, row).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(64 * kFltSplitWaves) filtered_maxima_kernel(FilteredArgs a, int chunks) {
+  __shared__ float m4[kFltSplitWaves][64];
+  const int r = blockIdx.x / chunks, c = blockIdx.x - r * chunks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  FilteredRow* row = (FilteredRow*)a.scratch + r;
+  const int base = (c * kFltSplitWaves + wave) * kLpTile;
+  float m = -INFINITY;
+  if (base < a.vocab) {
+    float v[16];
+    Tile<T, VEC>::load((const T*)a.logits + r * a.row_stride, base, a.vocab, lane, v);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, v[e]);
+  }
+  m4[wave][lane] = m;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < kFltSplitWaves; ++w) m = fmaxf(m, m4[w][lane]);
+  row->maxima[64 * c + lane] = m;
+  if (c == 0 && lane == 0) {
+    row->total = 0;
+    row->n = 0;
+    row->kept = 0;
+  }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(64 * kFltSplitWaves) filtered_list_kernel(FilteredArgs a, int chunks) {
+  constexpr int N = 64 * kFltSplitWaves, PER = kFltBins / N;
+  __shared__ uint32_t count[kFltBins];
+  __shared__ float wmax[kFltSplitWaves];
+  __shared__ uint32_t wsum[kFltSplitWaves];
+  __shared__ int last_bin;
+  const int r = blockIdx.x / chunks, c = blockIdx.x - r * chunks, tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  FilteredRow* row = (FilteredRow*)a.scratch + r;
+  const int base = (c * kFltSplitWaves + wave) * kLpTile;
+  float v[16];
+  if (base < a.vocab) Tile<T, VEC>::load((const T*)a.logits + r * a.row_stride, base, a.vocab, lane, v);
+  RowDraw rd(a, r);
+  float mx[kFltMaxima / N], m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kFltMaxima / N; ++i) {
+    const int at = tid + N * i;
+    mx[i] = at < 64 * chunks ? row->maxima[at] : -INFINITY;
+    m = fmaxf(m, mx[i]);
+  }
+  for (int i = tid; i < kFltBins; i += N) count[i] = 0;
+  if (tid == 0) last_bin = kFltBins - 2;
+  m = wave_max(m);
+  if (lane == 0) wmax[wave] = m;
+  __syncthreads();
+  m = wmax[0];
+#pragma unroll
+  for (int w = 1; w < kFltSplitWaves; ++w) m = fmaxf(m, wmax[w]);
+  rd.m = seen(m);
+  if (rd.m == -INFINITY) return;
+  if (rd.m == INFINITY) {
+    rd.m = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFltMaxima / N; ++i) mx[i] = mx[i] == INFINITY ? 0.f : -INFINITY;
+    read_infinite(v);
+  }
+  const bool whole = !rd.greedy && !rd.by_k && !rd.by_p;   // nothing but min-p filters
+  if (!whole && a.vocab > kFltList) {
+#pragma unroll
+    for (int i = 0; i < kFltMaxima / N; ++i) {
+      const int b = rd.bin(seen(mx[i]));
+      if (b < kFltBins - 1) atomicAdd(&count[b], 1u);
+    }
+    __syncthreads();
+    uint32_t own[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      own[i] = count[PER * tid + i];
+      sum += own[i];
+    }
+    uint32_t inc = wave_scan32(sum);
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) inc += wsum[w];
+    const uint32_t want = rd.greedy ? 1 : rd.by_k ? (uint32_t)rd.k : kFltThreads / 2;
+    uint32_t run = inc - sum;
+    if (run < want && want <= inc) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (run < want && want <= run + own[i]) last_bin = PER * tid + i;
+        run += own[i];
+      }
+    }
+    __syncthreads();
+  }
+  if (base >= a.vocab) return;
+  const float end = (float)(last_bin + 1);
+  uint64_t total = 0;
+  uint32_t in = 0, kept = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float l = seen(v[e]);
+    if (!whole && rd.place(l) < end) in |= 1u << e;
+    if (whole || !rd.by_k) {
+      const uint64_t w = whole && rd.weight_word(l) < rd.least ? 0 : rd.weight(l);
+      total += w;
+      kept += w != 0;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    total += shfl_xor_u64(total, o);
+    kept += __shfl_xor(kept, o, 64);
+  }
+  if (lane == 0) {
+    if (whole) {
+      row->tile[base / kLpTile] = total;
+      atomicAdd(&row->kept, kept);
+    } else if (!rd.by_k) {
+      atomicAdd((unsigned long long*)&row->total, (unsigned long long)total);
+    }
+  }
+  if (__any(in != 0)) {
+    // one reservation a wave: its lanes' entries one lane after the other
+    const uint32_t mine = __popc(in), inc = wave_scan32(mine);
+    uint32_t at = 0;
+    if (lane == 63) at = atomicAdd(&row->n, inc);
+    at = __shfl(at, 63, 64) + inc - mine;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (in >> e & 1) {
+        if (at < kFltList) row->list[at] = entry_word(seen(v[e]), Tile<T, VEC>::index(base, e, lane));
+        ++at;
+      }
+  }
+}
+
+// The split readings are made where the rows alone would leave CUs idle.
+static bool split_rows(int rows, int vocab) { return rows <= 128 && vocab > 2 * kFltWaves * kLpTile; }
+
 size_t sample_filtered_scratch(int rows, int vocab) {
-  (void)rows;
-  (void)vocab;
-  return 0;
+  return split_rows(rows, vocab) ? (size_t)rows * (sizeof(FilteredRow) / 4) : 0;
+}
+
+template <typename T, bool VEC>
+static void launch_filtered(const FilteredArgs& a, hipStream_t s) {
+  const dim3 grid(a.rows), block(kFltThreads);
+  if (split_rows(a.rows, a.vocab)) {
+    const int chunks = split_chunks(a.vocab);
+    const dim3 g2((unsigned)(a.rows * chunks)), b2(64 * kFltSplitWaves);
+    SR_LAUNCH((filtered_maxima_kernel<T, VEC>), g2, b2, 0, s, a, chunks);
+    SR_CHECK_LAUNCH();
+    SR_LAUNCH((filtered_list_kernel<T, VEC>), g2, b2, 0, s, a, chunks);
+    SR_CHECK_LAUNCH();
+    SR_LAUNCH((filtered_kernel<T, VEC, true>), grid, block, 0, s, a);
+  } else {
+    SR_LAUNCH((filtered_kernel<T, VEC, false>), grid, block, 0, s, a);
+  }
+  SR_CHECK_LAUNCH();
 }
 
 template <typename T>
-static void launch_filtered(const FilteredArgs& a, hipStream_t s) {
+static void by_alignment(const FilteredArgs& a, hipStream_t s) {
   const bool vec = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && (a.rows == 1 || a.row_stride * sizeof(T) % 16 == 0);
-  if (vec) SR_LAUNCH((filtered_kernel<T, true>), dim3(a.rows), dim3(kFltThreads), 0, s, a);
-  else SR_LAUNCH((filtered_kernel<T, false>), dim3(a.rows), dim3(kFltThreads), 0, s, a);
-  SR_CHECK_LAUNCH();
+  if (vec) launch_filtered<T, true>(a, s);
+  else launch_filtered<T, false>(a, s);
 }
 
 void sample_filtered(const FilteredArgs& a, hipStream_t s) {
   if (a.rows <= 0) return;
-  if (a.dtype == SR_BF16) launch_filtered<bf16_t>(a, s);
-  else launch_filtered<float>(a, s);
+  if (a.dtype == SR_BF16) by_alignment<bf16_t>(a, s);
+  else by_alignment<float>(a, s);
 }
 
 }  // namespace sr
