@@ -155,6 +155,38 @@ def test_borders_among_many_equals(vocab):
         check(torch, sr, t, what="equals", **s)
 
 
+@pytest.mark.parametrize("rows", [2, 140])
+def test_entries_down_to_weight_zero(rows):
+    """A top-k whose border lies where weights have run out: entries of weight 0 are
+    not counted as kept."""
+    torch, sr = need_gpu()
+    vocab = 40001
+    x = np.stack([-np.linspace(0, (22.1, 22.24, 22.3, 23.0, 30.0)[r % 5], vocab)[np.random.default_rng(r).permutation(vocab)]
+                  for r in range(rows)]).astype(np.float32)
+    for s in (dict(k=vocab - 1), dict(k=39900), dict(k=39900, p=1 - 2.0 ** -24), dict(k=20000), dict(p=1 - 2.0 ** -24), dict(k=39990, min_p=2.0 ** -31)):
+        check(torch, sr, torch.from_numpy(x).cuda(), what="ramp", **s)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_many_long_rows(bf16):
+    """More rows than have their readings shared out, each with settings of its own."""
+    torch, sr = need_gpu()
+    rng = np.random.default_rng(5)
+    rows, vocab = 150, 40000
+    x = np.concatenate([spread(rng, rows // 2, vocab, kind) for kind in ("flat", "peaked")]).astype(np.float32)
+    x[::9] = np.round(x[::9])
+    x[4::11, ::2] = -np.inf
+    x[5::13, rng.integers(0, vocab, 3)] = np.inf
+    x[6::17, rng.integers(0, vocab, 900)] = np.nan
+    x[[7, 70]] = -np.inf
+    x[[8, 80], 1:] = -np.inf
+    x = torch.from_numpy(x).cuda().to(torch.bfloat16 if bf16 else torch.float32)
+    f = lambda *v: rng.choice(np.array(v, np.float32), rows)  # noqa: E731
+    for _ in range(3):
+        check(torch, sr, x, f(0, 0.5, 1, 1.7), rng.choice(np.array([0, 1, 7, 300, 1024, 1025, 6000], np.int32), rows),
+              f(1, 0.3, 0.9, 0.99), f(0, 0, 0.02, 0.3), what="long")
+
+
 def test_odd_settings():
     """What is outside the usual ranges has its documented meaning."""
     torch, sr = need_gpu()
