@@ -40,10 +40,9 @@ enum { SR_FP4 = 2 };
  * head, and for caches of 4 bits.  q_gain, k_gain: DEVICE float [head_dim] or
  * NULL (no norm there); a head x becomes x / sqrt(mean(x^2) + eps) * gain, all
  * head_dim dimensions, before the first rot_dim of them are rotated.  cache:
- * SR_F32, SR_BF16 or SR_FP4, the type of kpool and vpool.  Keys are computed in 64
- * bits and rounded once, so that what a cache holds does not turn on the order of
- * a sum; queries in 32 bits behind angles, sines and cosines in 64.  Everything
- * else (qkv, freqs, tables, n_new, tokens without a page, limits) is as
+ * SR_F32, SR_BF16 or SR_FP4, the type of kpool and vpool.  Everything is computed
+ * in 64 bits and rounded once, so that what a cache holds does not turn on the order
+ * of a sum.  Everything else (qkv, freqs, tables, n_new, tokens without a page, limits) is as
  * sr_page_append has it.  eps >= 0 and finite; with eps = 0 a head of zeros gives
  * NaN. */
 sr_status sr_page_append_norm(int32_t cache, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
@@ -73,8 +72,9 @@ sr_status sr_page_read(int32_t cache, int32_t dtype, int32_t head_dim, int32_t n
  * operands are bf16: keys and values enter them exactly.  SR_BF16: queries keep 16
  * bits where a row has at most 16 query columns (lr n_heads / n_kv_heads) and 8
  * where it has more, probabilities 8, sums are in fp32.  SR_F32: queries and
- * probabilities enter as three parts, all 24 bits.  scratch: DEVICE float of
- * scratch_elems >= sr_paged_attention_fp4_scratch(...) elements. */
+ * probabilities enter as three parts, all 24 bits.  A layer's keys take less than
+ * 2^36 bytes.  scratch: DEVICE float of scratch_elems >=
+ * sr_paged_attention_fp4_scratch(...) elements. */
 sr_status sr_paged_attention_fp4(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,
                                  int32_t rows, int32_t lr, const float *q, const void *kpool,
                                  const void *vpool, int32_t page_tokens, int32_t n_pages,

@@ -117,10 +117,11 @@ __device__ __forceinline__ __bf16 my_part(float x, int part) {
 //   O^T += V^T P^T (v_mfma_f32_16x16x32_bf16): a V block is converted on its way into
 //         LDS (the wave's own) and its A operand comes from two transpose reads; the
 //         contraction visits the keys in the order the lane holds their probabilities.
-// A block's registers take over the next block as soon as they are read.  A block's 16-key halves lie in one page each; lane i holds
-// the places and flags of block i of a run of 64.  The keys below common[row] are
-// another pass's.  Keys that nobody sees are read where they lie (their scores are
-// masked) and their values as zeros; a half without a page is read from page 0.
+// A block's registers take over the next block as soon as they are read.  A block's
+// 16-key halves lie in one page each; lane i holds the places and flags of block i of a
+// run of 64.  The keys below common[row] are another pass's.  Keys that nobody sees are
+// read where they lie (their scores are masked) and their values as zeros; a half
+// without a page is read from page 0.
 template <int HD, int NW, bool F32, int SPREAD>
 __global__ void __launch_bounds__(64 * NW, HD == 128 && SPREAD == 1 ? 3 : 4)
 fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
@@ -862,35 +863,53 @@ struct Fp4Plan {
   int slots() const { return pre + (splits > 1 ? splits : 0); }
 };
 
-constexpr int kTileTarget = 512;
-constexpr int kMaxSplits = 64;
-static int tile_splits(int64_t groups, int64_t blocks) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({kTileTarget / groups, blocks / 8, kMaxSplits}));
+// How often fp4_wave_kernel has a column in its 16.
+static int wave_spread(const PagedAttnArgs& a) {
+  const int cols = a.lr * (a.hq / a.hkv), times = a.dtype == SR_BF16 ? 2 : 4;
+  return cols * times <= 16 ? times : 1;
 }
-constexpr int kWaveTarget = 3072;
-constexpr int64_t kShareBytes = 300 << 20;
+
+// Single tokens: as many waves as are resident at once (3 or 4 a SIMD, a wave having
+// four blocks of keys at least), no more, since what does not fit waits for a whole
+// round.  256 rows of 612 keys, hd 128: 2048 waves of several work-groups a row 36 us,
+// 4096 31 us, 8192 35 us; 5 rows of 30-60k: 59.5, 60, 64 us; 200 rows of 700 in fp32,
+// two blocks a wave: 16.5 us, four: 12.9 us.
+constexpr int kSimds = 1024;
+// Tiles: two work-groups a CU (20 tokens on 60k keys: one 65 us, two 51 us); for the
+// shared keys one, since another split is another set of partials to write and read
+// (512 rows, 1024 shared keys: two 73 us, one 71 us, half of the CUs 82 us).
+constexpr int kTileTarget = 512, kPreTarget = 256;
+// Bytes of the shared keys and values as often as rows read them, from which they get a
+// pass of their own (1024 shared and 100-300 own keys of 8 heads of 128 dimensions: 128
+// rows 34 us with it, 30 without, 192 rows 36 and 43, 512 rows 71 and 94; 512 rows with
+// 256 shared 48 and 42, with 512 51 and 56).
+constexpr int64_t kShareBytes = 190 << 20;
+constexpr int kMaxSplits = 64;
 
 static Fp4Plan fp4_plan(const PagedAttnArgs& a) {
   Fp4Plan p{false, 1, 1, 0};
   const int g = a.hq / a.hkv;
   int64_t keys = planned_keys(a);
+  auto tile_splits = [&](int64_t groups, int64_t blocks, int target) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({target / groups, blocks / 8, kMaxSplits}));
+  };
   if (a.lr * g <= 16) {
     const bool far = a.window > 0 && a.max_len > a.window;   // (windows have left key 0)
     const int64_t shared = far ? 0 : std::min<int64_t>(a.shared, keys - a.lr);
     if (shared > 0 && (int64_t)a.rows * shared * a.hkv * a.hd * 17 / 16 >= kShareBytes) {
       const int64_t tiles = ((int64_t)a.rows * a.lr * g + kTileCols - 1) / kTileCols;
-      p.pre = tile_splits(tiles * a.hkv, shared / 32);
+      p.pre = tile_splits(tiles * a.hkv, shared / 32, kPreTarget);
       keys -= shared;
     }
     const int64_t pairs = (int64_t)a.rows * a.hkv, blocks = (keys + 31) / 32;
-    int64_t want = std::max<int64_t>(1, std::min<int64_t>(kWaveTarget / pairs, blocks / 2));
-    if (want > 8 && pairs * 8 >= 1024) want = 8;
+    const int resident = a.hd == 128 && wave_spread(a) == 1 ? 3 : 4;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(resident * kSimds / pairs, blocks / 4));
     p.nw = want >= 4 ? 4 : want >= 2 ? 2 : 1;
-    p.splits = (int)std::min<int64_t>(kMaxSplits, (want + p.nw - 1) / p.nw);
+    p.splits = (int)std::min<int64_t>(kMaxSplits, want / p.nw);
   } else {
     p.tile = true;
     const int64_t tiles = ((int64_t)a.lr * g + kTileCols - 1) / kTileCols;
-    p.splits = tile_splits(tiles * a.hkv * a.rows, keys / 32);
+    p.splits = tile_splits(tiles * a.hkv * a.rows, keys / 32, kTileTarget);
   }
   return p;
 }
@@ -932,13 +951,12 @@ static void launch_fp4(const PagedAttnArgs& a, hipStream_t s) {
       launch_tile<HD, true, F32>(a, common, p.pre, p.slots(), s);
     }
     const dim3 grid(p.splits, a.hkv, a.rows);
-    const int cols = a.lr * (a.hq / a.hkv);
 #define SR_FP4_WAVE2(NW, SPREAD)                                                                                    \
   SR_LAUNCH((fp4_wave_kernel<HD, NW, F32, SPREAD>), grid, dim3(64 * NW), 0, s, a, (const int32_t*)common, p.splits, \
             p.pre, p.slots(), qscale)
 #define SR_FP4_WAVE(NW)                                         \
   do {                                                          \
-    if (cols <= (F32 ? 4 : 8)) SR_FP4_WAVE2(NW, (F32 ? 4 : 2)); \
+    if (wave_spread(a) > 1) SR_FP4_WAVE2(NW, (F32 ? 4 : 2));    \
     else SR_FP4_WAVE2(NW, 1);                                   \
   } while (0)
     switch (p.nw) {

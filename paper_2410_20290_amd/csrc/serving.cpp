@@ -127,6 +127,7 @@ sr_status sr_paged_attention_fp4(int32_t dtype, int32_t head_dim, int32_t n_head
     require(aligned16(scratch), "scratch must be 16-byte aligned");
     const int64_t heads = (int64_t)rows * lr * n_heads * head_dim;
     const int64_t block = cache_bytes(SR_FP4, n_pages, n_kv_heads, a.shift, head_dim);
+    supported(block >> 36 == 0, "a layer's keys of 64 GB or more");   // (the kernels hold places in 16 bytes, 32 bits)
     const Range in[] = {{q, 4 * heads}, {kpool, block}, {vpool, block}, {table, 4 * (int64_t)rows * max_pages},
                         {lens, 4 * (int64_t)rows}, {n_new, 4 * (int64_t)rows}};
     const Range dst[] = {{out, heads * (dtype == SR_BF16 ? 2 : 4)}, {need ? scratch : nullptr, 4 * (int64_t)need}};

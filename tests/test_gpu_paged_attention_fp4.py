@@ -130,6 +130,54 @@ def test_shared_pages(bf16, hd, hq, hkv, rows, shared):
     case(21, bf16, hd, hq, hkv, lens, 1, 32, shared=0, shared_arg=shared)   # nothing in common
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 16, 8), (64, 8, 4), (128, 6, 2)])
+def test_shared_pages_of_many_rows(bf16, hd, hq, hkv):
+    """So many that the shared keys are read once for all rows; some rows share less
+    than the others, or nothing."""
+    rng = np.random.default_rng(6)
+    rows, shared, pt = 512, 2048, 64
+    lens = [shared + int(n) for n in rng.integers(1, 90, rows)]
+    lens[3], lens[4], lens[5], lens[6] = 700, 5, 0, shared
+    new = [int(n) for n in rng.integers(0, 3, rows)]
+    holes = {(7, 0): -1, (8, 3): -1, (9, 31): -1}
+    case(30, bf16, hd, hq, hkv, lens, 1, pt, shared=shared, holes=holes)
+    case(31, bf16, hd, hq, hkv, lens, 2, pt, shared=shared, n_new=new)
+
+
+def test_pools_past_32_bits():
+    """Pages that lie past 2^32 bytes of a pool hold what is put there, and are read
+    from there: as a small pool of the same tokens, bit for bit."""
+    torch, sr = need_gpu()
+    say("pools past 2^32 bytes")
+    rng = np.random.default_rng(9)
+    hd, hq, hkv, pt, rows, lr, mp = 128, 8, 8, 256, 3, 300, 3
+    n_pages = (1 << 32) // (hkv * pt * sr.fp4_token_bytes(hd)) + 40
+    far = n_pages - 1 - np.arange(rows * mp, dtype=np.int32).reshape(rows, mp)
+    near = far - far.min()
+    lens = torch.tensor([700, 301, 300], dtype=torch.int32, device="cuda")
+    qkv = torch.from_numpy(rng.normal(size=(rows, 700, (hq + 2 * hkv) * hd)).astype(np.float32)).cuda()
+    got = []
+    for table, n in ((near, rows * mp), (far, n_pages)):
+        k, v = (torch.empty((n, hkv, pt, sr.fp4_token_bytes(hd)), dtype=torch.uint8, device="cuda") for _ in range(2))
+        t = torch.from_numpy(table.astype(np.int32)).cuda()
+        q = torch.zeros((rows, 700, hq, hd), device="cuda")
+        sr.page_append_norm(qkv, None, t, lens, k, v, q, n_new=lens)
+        ko, vo = (torch.zeros((rows, 700, hkv, hd), device="cuda") for _ in range(2))
+        sr.page_read(k, v, t, lens, ko, vo, n_new=lens)
+        outs = [ko, vo]
+        for m in (1, lr):
+            for typ in (torch.bfloat16, torch.float32):
+                o = torch.zeros((rows, m, hq * hd), dtype=typ, device="cuda")
+                sr.paged_attention_fp4(q[:, :m].contiguous(), k, v, t, lens, o)
+                outs.append(o)
+        torch.cuda.synchronize()
+        got.append([x.cpu() for x in outs])
+        del k, v
+    assert float(got[0][0].abs().max()) > 1 and all(float(x.float().abs().max()) > 0 for x in got[0])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_nan_and_infinities():
     """A group with byte 255 gives NaN in the outputs that depend on it and in no
     others, in a key and in a value; a NaN query too."""

@@ -87,7 +87,13 @@ ATTN = dict(dtype=sr.SR_BF16, hd=64, hq=8, hkv=2, rows=2, lr=3, q=0x700000, k=0x
     (dict(dtype=2), INVALID), (dict(hq=7), INVALID), (dict(q=None), INVALID), (dict(q=0x700004), INVALID),
     (dict(hq=34), UNSUPPORTED), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID), (dict(shared=-1), INVALID),
     (dict(max_len=0), INVALID), (dict(out=None), INVALID), (dict(out=0x800002), INVALID), (dict(out=0x700000), INVALID),
-    (dict(out=0x300000), INVALID), (dict(rows=4096, lr=1 << 16), UNSUPPORTED)])
+    (dict(out=0x300000), INVALID), (dict(rows=4096, lr=1 << 16), UNSUPPORTED),
+    # 2^20 pages of 256 tokens, 8 heads of 128 dimensions: 146 GB
+    (dict(n_pages=1 << 20, pt=256, hd=128, hq=8, hkv=8), UNSUPPORTED),
+    (dict(rows=1, lr=1, mp=4096, max_len=65536, n=64), SMALL), (dict(rows=1, lr=1, mp=4096, max_len=65536, scratch=None), SMALL),
+    (dict(rows=1, lr=1, mp=4096, max_len=65536, scratch=0x10000008), INVALID),
+    (dict(rows=1, lr=1, mp=4096, max_len=65536, scratch=0x800000), INVALID),
+    (dict(rows=512, lr=1, mp=256, max_len=4096, shared=2048, hkv=8, n=512), SMALL)])
 def test_attention_refuses(L, kw, status):
     assert L.sr_paged_attention_fp4(*args(ATTN, kw)) == status and sr.last_error()
 
@@ -112,7 +118,10 @@ DRAW = dict(dtype=sr.SR_F32, logits=0x100000, stride=1000, rows=2, vocab=1000, T
     (dict(vocab=262145, stride=262145), UNSUPPORTED), (dict(rows=(1 << 20) + 1), UNSUPPORTED), (dict(logits=None), INVALID),
     (dict(random=None), INVALID), (dict(rstride=-1), INVALID), (dict(logits=0x100002), INVALID), (dict(T=0x600002), INVALID),
     (dict(k=0x600001), INVALID), (dict(token=0x100000), INVALID), (dict(lp=0x300004), INVALID), (dict(kept=0x200004), INVALID),
-    (dict(token=0x600000, T=0x600004), INVALID), (dict(lp=0x600000, m=0x600000), INVALID), (dict(stride=(1 << 40) + 1), UNSUPPORTED)])
+    (dict(token=0x600000, T=0x600004), INVALID), (dict(lp=0x600000, m=0x600000), INVALID), (dict(stride=(1 << 40) + 1), UNSUPPORTED),
+    (dict(rows=1, vocab=128256, stride=128256, n=3), SMALL), (dict(rows=1, vocab=128256, stride=128256, scratch=None), SMALL),
+    (dict(rows=1, vocab=128256, stride=128256, scratch=0x10000004), INVALID),
+    (dict(rows=1, vocab=128256, stride=128256, scratch=0x300000), INVALID)])
 def test_draw_refuses(L, kw, status):
     assert L.sr_sample_filtered(*args(DRAW, kw)) == status and sr.last_error()
 
