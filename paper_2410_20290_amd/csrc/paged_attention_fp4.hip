@@ -29,6 +29,10 @@
 
 namespace sr {
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
+
 constexpr float kStale = 8.f;
 
 // Eight codes (a word, the lowest first) times a scale, as bf16.
@@ -463,21 +467,33 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 // The 32-key blocks that hold a visible key pass through registers, two blocks
 // ahead, and are converted on their way into one of two LDS stages (every thread 8 or
 // 16 dimensions of a key and of a value, rows XOR-swizzled in chunks of 16 bytes); one
-// barrier a block.  Lane i keeps the place and the mask flags of block i of a
-// run of 64.  The output is rescaled only when a maximum has moved by more than
+// barrier a block.
+//   CODES (bf16 outputs of prompts): keys are not converted.  S^T is v_mfma_scale_f32_
+//                 32x32x64 on their codes and scale bytes, times queries in three parts of
+//                 6 bits (e2m3), each with a scale for 32 dimensions: 2^-14 of the
+//                 largest of these is left, and products are cut at some 2^-14 of a
+//                 group's largest.  6011 tokens, hd 128: 323 us, 917 TFLOP/s; queries in
+//                 one bf16 341 us and with twice the error, in two 537 us.  53 chunks of
+//                 up to 333 tokens, hd 64: 150, 134 and 166 us.
+// What bounds it: a block of 32 x 32 scores is 256 clocks of exponentials and some 250
+// of other vector work a wave, beside 512 (hd 128) of matrix work.  Lane i keeps the place and the mask flags of block i of a run of 64.
+// The output is rescaled only when a maximum has moved by more than
 // kStale.
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE, bool F32>
-__global__ void __launch_bounds__(256, PRE || F32 ? 2 : 3)
+__global__ void __launch_bounds__(256, HD == 128 || PRE || F32 ? 2 : 3)
 fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slots, float qscale) {
   constexpr int KT = 32, NW = 4;
   constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
-  constexpr int QP = F32 ? 3 : PRE ? 2 : 1, PP = F32 ? 3 : 1;
+  constexpr bool CODES = !F32 && !PRE;         // scores from the codes themselves
+  constexpr int PP = F32 ? 3 : 1, QP = PRE && !F32 ? 2 : 3;   // parts of a probability, of a query
+  constexpr int GS = HD / 32, LJ = (HD + 63) / 64;   // groups of a key, products over these
   constexpr int TILE = KT * HD;                // bf16 elements of a K (or V) block
   constexpr int TPK = HD == 32 ? 4 : 8;        // threads that bring a key
   constexpr int WPT = CPK / TPK;               // chunks (words of codes) of each
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2 * 2 * TILE];
+  __shared__ __attribute__((aligned(16))) uint8_t raw[2][CODES ? KT * 16 * GS : 16], raw_scale[2][CODES ? KT * 4 : 4];
   __shared__ int bounds[NW][2];
   // a 1-D grid dealt round-robin to the 8 XCDs: each takes consecutive logical
   // blocks, the query tiles of one (row, KV head, split) fastest, the last and
@@ -611,15 +627,23 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   read_table(0);
   __builtin_amdgcn_sched_barrier(0);
 
-  // The wave's 32 queries, 16 bytes per lane along whole rows (clamped rows;
-  // results of columns that are no query are dropped)
+  // The wave's 32 queries (clamped rows; results of columns that are no query are
+  // dropped).  For CODES a lane takes dimensions 64 j + 32 fh .. of its column (32
+  // dimensions: the lower half), else 16 bytes along whole rows.
   constexpr int LPR = HD / 4, RPQ = 64 / LPR, NQ = 32 / RPQ;   // lanes per query, queries per load, loads
-  float4 qv[NQ];
+  float4 qv[CODES ? 8 * LJ : NQ];
+  if constexpr (CODES) {
+    const int x = imin(xw + fr, X - 1), tok = x / g;
+    const float4* src = reinterpret_cast<const float4*>(a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD);
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int x = imin(xw + RPQ * i + lane / LPR, X - 1), tok = x / g;
-    qv[i] = reinterpret_cast<const float4*>(
-        a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
+    for (int i = 0; i < 8 * LJ; ++i) qv[i] = src[i % 8 + (HD == 32 ? 0 : 16 * (i / 8) + 8 * fh)];
+  } else {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int x = imin(xw + RPQ * i + lane / LPR, X - 1), tok = x / g;
+      qv[i] = reinterpret_cast<const float4*>(
+          a.q + ((int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g)) * HD)[lane % LPR];
+    }
   }
   __builtin_amdgcn_sched_barrier(0);
 
@@ -645,6 +669,8 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     c.ks = ((const uint8_t*)a.kpool + off + scales)[owns];
     c.vs = ((const uint8_t*)a.vpool + off + scales)[owns];
   };
+  // 16 bytes of codes of key k in a stage: 16 lanes' reads meet in no bank
+  auto raw_slot = [](int k, int group) { return k * GS + (group ^ (HD == 128 ? (k >> 2) & 3 : HD == 64 ? (k >> 3) & 1 : 0)); };
   auto vswz = [](int k) { return HD == 128 ? (k & 3) << 2 : HD == 64 ? ((k >> 1) & 1) << 2 : 0; };
   auto stage = [&](int tile, Codes& c, int buf) {
     if (HD == 32 && !brings) return;
@@ -657,12 +683,22 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     const float ks = fp4_scale(c.ks), vs = fp4_scale(c.vs);
 #pragma unroll
     for (int w = 0; w < WPT; ++w) {
-      *reinterpret_cast<bf16x8*>(kd + 8 * ((chunk + w) ^ (key & (CPK - 1)))) = fp4_to_bf16(c.k[w], ks);
+      if constexpr (!CODES) *reinterpret_cast<bf16x8*>(kd + 8 * ((chunk + w) ^ (key & (CPK - 1)))) = fp4_to_bf16(c.k[w], ks);
       *reinterpret_cast<bf16x8*>(kd + TILE + 8 * ((chunk + w) ^ vswz(key))) = fp4_to_bf16(c.v[w], vs);
+    }
+    if constexpr (CODES) {
+      uint32_t* dst = reinterpret_cast<uint32_t*>(raw[buf] + 16 * raw_slot(key, chunk / 4)) + chunk % 4;
+#pragma unroll
+      for (int w = 0; w < WPT; ++w) dst[w] = c.k[w];
+      if (chunk % 4 == 0) raw_scale[buf][4 * key + chunk / 4] = c.ks;
     }
   };
 
-  bf16x8 qf[QP][KS];   // the queries' parts
+  // the queries' parts: of 6 bits, groups of 32 dimensions with a scale byte (part p's of
+  // product j: byte 2 p + j of the two words), or bf16
+  u32x6 q6[CODES ? QP : 1][LJ];
+  uint32_t q6_scale[2] = {0, 0};
+  bf16x8 qf[CODES ? 1 : QP][KS];
   // byte offset in a stage of chunk fh of K row fr (chunk 2 s + fh: this ^ 32 s)
   const uint32_t kbase = (uint32_t)(fr * HD + 8 * (fh ^ (fr & (CPK - 1)))) * 2;
   // LDS address in the first V block of dims 16 (l / 16 % 2) + 4 (l % 4) .. of key
@@ -693,11 +729,36 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     f32x16 sc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+    if constexpr (CODES) {
+      // key fr's codes, and the scale bytes from the lane's first group on (32 dimensions:
+      // the queries are 0 in the other half, where the codes stand in for themselves)
+      const uint32_t ks = *reinterpret_cast<const uint32_t*>(raw_scale[ST] + 4 * fr) >> (HD == 32 ? 0 : 8 * fh);
+      i32x8 k[LJ];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const bf16x8 k = frag(lds + ST * 2 * TILE, s);
+      for (int j = 0; j < LJ; ++j) {
+        const uint4 v = *reinterpret_cast<const uint4*>(raw[ST] + 16 * raw_slot(fr, HD == 32 ? 0 : 2 * j + fh));
+        k[j] = i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+      }
+      auto part = [&](auto p) {
+        constexpr int P = decltype(p)::value;
+        auto q = [&](int j) {
+          const u32x6 w = q6[P][j];
+          return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
+        };
+        sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[0], q(0), sc, 4, 2, 0, ks, 2 * (P & 1), q6_scale[P / 2]);
+        if constexpr (LJ == 2)
+          sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[LJ - 1], q(LJ - 1), sc, 4, 2, 2, ks, 2 * (P & 1) + 1, q6_scale[P / 2]);
+      };
+      part(std::integral_constant<int, 2>{});   // (the least first)
+      part(std::integral_constant<int, 1>{});
+      part(std::integral_constant<int, 0>{});
+    } else {
 #pragma unroll
-      for (int i = 0; i < QP; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[i][s], sc, 0, 0, 0);
+      for (int s = 0; s < KS; ++s) {
+        const bf16x8 k = frag(lds + ST * 2 * TILE, s);
+#pragma unroll
+        for (int i = 0; i < QP; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[i][s], sc, 0, 0, 0);
+      }
     }
     if (f & EDGE) {                            // (uniform)
       asm volatile("");                        // (a branch, not selects on every block)
@@ -763,24 +824,65 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     Codes c0, c1;
     load(0, c0);
     if (ntile > 1) load(1, c1);
-    // (through the wave's own slice: its LDS operations are in order)
+    if constexpr (CODES) {
 #pragma unroll
-    for (int p = 0; p < QP; ++p) {
+      for (int j = 0; j < LJ; ++j) {
+        float x[32], top = 0.f;
+        bool fine = true;
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
-        const float x[4] = {qv[i].x * qscale, qv[i].y * qscale, qv[i].z * qscale, qv[i].w * qscale};
-        bf16x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          __bf16 part[QP];
-          in_parts<QP>(x[e], part);
-          v[e] = part[p];
+        for (int i = 0; i < 8; ++i) {
+          const float4 v = qv[8 * j + i];
+          x[4 * i] = v.x * qscale; x[4 * i + 1] = v.y * qscale; x[4 * i + 2] = v.z * qscale; x[4 * i + 3] = v.w * qscale;
         }
-        *reinterpret_cast<bf16x4*>(slice + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
-      }
 #pragma unroll
-      for (int s = 0; s < KS; ++s) qf[p][s] = frag(slice, s);
+        for (int e = 0; e < 32; ++e) {
+          if (HD == 32 && fh) x[e] = 0.f;
+          fine &= fabsf(x[e]) <= FLT_MAX;
+          top = fmaxf(top, fabsf(x[e]));
+        }
+#pragma unroll
+        for (int p = 0; p < QP; ++p) {
+          // the least scale with the largest at most 7.5 of it, the type's end
+          const int byte = imax(1, (int)((__float_as_uint(top) + 0xFFFFFu) >> 23) - 2);
+          const float scale = __uint_as_float((uint32_t)byte << 23);
+          f32x16 even, odd;   // (whose results alternate)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            even[e] = x[2 * e];
+            odd[e] = x[2 * e + 1];
+          }
+          q6[p][j] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+          q6_scale[p / 2] |= (uint32_t)(fine ? byte : 255) << (8 * (2 * (p & 1) + j));   // (255: NaN)
+          if (p + 1 == QP) break;
+          const f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q6[p][j], scale);
+          top = 0.f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            x[e] -= y[e];
+            top = fmaxf(top, fabsf(x[e]));
+          }
+        }
+      }
+    } else {
+      // (through the wave's own slice: its LDS operations are in order)
+#pragma unroll
+      for (int p = 0; p < QP; ++p) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const int r = RPQ * i + lane / LPR, c4 = lane % LPR;
+          const float x[4] = {qv[i].x * qscale, qv[i].y * qscale, qv[i].z * qscale, qv[i].w * qscale};
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            __bf16 part[QP];
+            in_parts<QP>(x[e], part);
+            v[e] = part[p];
+          }
+          *reinterpret_cast<bf16x4*>(slice + r * HD + 8 * ((c4 >> 1) ^ (r & (CPK - 1))) + 4 * (c4 & 1)) = v;
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[p][s] = frag(slice, s);
+      }
     }
     lds_barrier();   // every wave's queries read
     // Block t is staged, its registers take block t + 2, and behind the barrier all

@@ -76,8 +76,14 @@ def attention(cache, q, n_new, window, sinks, bf16):
     cache, and how far roundings may move each element.
 
     Keys and values are exact.  bf16: queries enter the products with a relative
-    error of 2^-16 where a row has at most 16 columns (two halves, 2^-8 each) and 2^-8
-    where it has more; probabilities with 2^-8; the output is rounded, 2^-8.  fp32:
+    error of 2^-16 where a row has at most 16 columns (two halves, 2^-8 each).  Where it
+    has more they enter as three parts of 6 bits (steps of 1/8 up to 2, 1/4 up to 4, 1/2 up to 7.5), each times a
+    power of two s for 32 dimensions, the least with which the largest is at most 7.5 s,
+    so above 3.75 s: the first part leaves at most s / 4, which is at most 4 of the
+    second's steps of scale s / 16, so that leaves s / 128, and the third s / 4096, below
+    2^-13 of the largest of the 32; the products of such a group are cut at some 2^-14
+    of the largest of them, another 2^-13 of that sum of magnitudes: 2^-12 together.
+    Probabilities enter with 2^-8; the output is rounded, 2^-8.  fp32:
     three parts, 2^-24, and 2^-24 each.  A score adds up hd products (and their
     parts: three times as many, each step 2^-24 of the sum of magnitudes) and a
     factor; so it moves by d and a probability by a factor within e^(2 d); the
@@ -88,7 +94,8 @@ def attention(cache, q, n_new, window, sinks, bf16):
     g = hq // cache.hkv
     U = 2.0 ** -24
     out, bound = np.zeros(q.shape), np.zeros(q.shape)
-    step = (2.0 ** -16 if lr * g <= 16 else 2.0 ** -8) if bf16 else U
+    step = 2.0 ** -16 if bf16 else U
+    grouped = bf16 and lr * g > 16
     last = 2.0 ** -8 if bf16 else U
     for r in range(rows):
         k, v, there = cache.rows_kv(r)
@@ -105,6 +112,9 @@ def attention(cache, q, n_new, window, sinks, bf16):
                 p /= p.sum(1, keepdims=True)
                 o = p @ vs
                 d = (step + (3 * hd + 4) * U) * (np.abs(qh) @ np.abs(ks).T).max(1) / np.sqrt(hd)
+                if grouped:
+                    top = np.repeat(np.abs(qh).reshape(g, -1, 32).max(2), 32, axis=1)
+                    d += 2.0 ** -12 * (top @ np.abs(ks).T).max(1) / np.sqrt(hd)
                 rel = np.expm1(2 * d) + last + 2 * (3 * see.sum() + 8) * U
                 low = see.sum() * 2.0 ** -123 * max(1.0, np.abs(vs).max())
                 out[r, t, h * g:(h + 1) * g] = o

@@ -59,8 +59,8 @@ def case(seed, bf16, hd, hq, hkv, lens, lr, pt, window=0, sinks=0, n_new=None, s
     ref, bound = attention(cache, q, new, window, sinks, bf16)
     # fp32: a score of magnitude s = sum |q k| / sqrt(hd), up to 100 here, is some 2^-23
     # s off, and a probability by that, 2^-17; bf16: the output's and the
-    # probabilities' roundings, 2^-9 each in the mean square at most, and with more
-    # than 16 columns the queries', 2^-9 s of a random walk over hd terms, 2^-9 |q| |k| / hd
+    # probabilities' roundings, 2^-9 each in the mean square at most; with more than 16
+    # columns scores are off by some 2^-13 of s too, as their queries are
     check(out, ref, bound, new, 2.0 ** -17 if not bf16 else 2.0 ** -8 if lr * hq // hkv <= 16 else 2.0 ** -6)
 
 
@@ -143,6 +143,38 @@ def test_shared_pages_of_many_rows(bf16, hd, hq, hkv):
     holes = {(7, 0): -1, (8, 3): -1, (9, 31): -1}
     case(30, bf16, hd, hq, hkv, lens, 1, pt, shared=shared, holes=holes)
     case(31, bf16, hd, hq, hkv, lens, 2, pt, shared=shared, n_new=new)
+
+
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
+@pytest.mark.parametrize("lr", [2, 70])
+def test_what_queries_keep_beyond_a_bf16(hd, hq, hkv, lr):
+    """Every token sees two keys, and its queries, 30 times as large as the keys, lie
+    almost across their difference: rounding the queries to bf16 moves the output more
+    than all other roundings.  What the kernel keeps beyond that (another 8 bits, or
+    parts of 6 bits in groups, some 2^-14 of a group's largest) has to take at least three
+    quarters of it away, beside the probabilities' and the output's 2^-9 each in the mean square."""
+    rng = np.random.default_rng(hd)
+    lens = [200, 131]
+    cache = Cache4(rng, lens, 16, hkv, hd)
+    q = 30 * rng.normal(size=(2, lr, hq, hd))
+    for r in range(2):
+        k = cache.rows_kv(r)[0]
+        for t in range(lr):
+            pos = lens[r] - lr + t
+            diff = np.repeat(k[pos] - k[pos - 1], hq // hkv, axis=0)
+            q[r, t] += ((rng.normal(size=hq) * np.sqrt(hd) - (q[r, t] * diff).sum(1)) / (diff * diff).sum(1))[:, None] * diff
+    q = q.astype(np.float32)
+    ref, _ = attention(cache, q, [lr, lr], 2, 0, True)
+    half = ((q.view(np.uint32) + 0x7FFF + ((q.view(np.uint32) >> 16) & 1)) & 0xFFFF0000).view(np.float32)
+    short, _ = attention(cache, half, [lr, lr], 2, 0, True)
+    size = np.linalg.norm(ref)
+    lost = np.linalg.norm(short - ref) / size
+    assert lost > 2.0 ** -6                                     # (or there is nothing to see)
+    torch, sr = need_gpu()
+    say(f"attention over 4 bits, precision of queries hd={hd} lr={lr}")
+    cache.poison([lr, lr], 2, 0)
+    out, _ = run(torch, sr, cache, q, [lr, lr], True, 2, 0)
+    assert np.linalg.norm(out - ref) / size <= np.hypot(lost / 4, np.sqrt(2) * 2.0 ** -9)
 
 
 def test_pools_past_32_bits():
