@@ -90,6 +90,11 @@ __device__ __forceinline__ int wslot(int k, int c) {
   else return vslot<CPK>(k, c);
 }
 
+// What all lanes hold alike, told to the compiler, which else keeps what comes of a
+// division or a load in vector registers, and loops over it by masks.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ RowState uniform(const RowState& r) { return {uniform(r.len), uniform(r.n), uniform(r.p0)}; }
+
 // ------------------------------------------------------- waves split keys
 // Query columns of a work-group and where their parts go: with up to 8 (4) columns each
 // is there SPREAD = 2 (4) times, and the matrix columns hold a part each, at no
@@ -138,7 +143,7 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   constexpr int BYTES = NW * 16 * ROW * 4 > NW * VB * 2 ? NW * 16 * ROW * 4 : NW * VB * 2;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[BYTES / 2];
   const int split = blockIdx.x, h = blockIdx.y, row = blockIdx.z;
-  const RowState rs = row_state(a, row);
+  const RowState rs = uniform(row_state(a, row));
   if (rs.n == 0) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -150,9 +155,11 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   const int end_c = rs.p0 + (live ? t : 0) + 1, lo_c = window_start(end_c - 1, a.window);
   const int lo_last = window_start(rs.len - 1, a.window);
   KeyBlocks kb;
-  kb.set(common ? common[row] : 0, a.sinks, window_start(rs.p0, a.window), rs.len);
+  kb.set(common ? uniform(common[row]) : 0, a.sinks, window_start(rs.p0, a.window), rs.len);
+  // (counts below 2^19, at most 256 shares)
   const int shares = splits * NW, me = split * NW + wave;
-  const int i0 = (int)((int64_t)kb.count * me / shares), i1 = (int)((int64_t)kb.count * (me + 1) / shares);
+  const int i0 = uniform((uint32_t)(kb.count * me) / (uint32_t)shares);
+  const int i1 = uniform((uint32_t)(kb.count * (me + 1)) / (uint32_t)shares);
   const int32_t* tab = a.table + (int64_t)row * a.max_pages;
   const int mask = (1 << a.shift) - 1;
   bf16_t* vbuf = lds + wave * VB;
@@ -506,17 +513,15 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   const int per_xcd = (total + 7) / 8;
   const int pid = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if (pid >= total) return;
-  const int qg = ngq - 1 - pid % ngq;
-  const int split = pid / ngq % splits;
   const int nrow = PRE ? 1 : a.rows;
-  const int row = pid / (ngq * splits) % nrow;
-  const int h = pid / (ngq * splits * nrow);
+  const int qg = uniform(ngq - 1 - pid % ngq), split = uniform(pid / ngq % splits);
+  const int row = uniform(pid / (ngq * splits) % nrow), h = uniform(pid / (ngq * splits * nrow));
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fh = lane >> 5;
   const int x0 = qg * kTileCols, xw = x0 + 32 * wave;             // first column, of the wave too
   const int token0 = PRE ? 0 : row * a.lr;
-  const RowState rs = row_state(a, row);
+  const RowState rs = uniform(row_state(a, row));
   if (!PRE && x0 >= rs.n * g) return;
 
   // This lane's column sees keys [0, sinks) and [lo, end); the wave's columns
@@ -564,8 +569,8 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   } else {
     const int last = imin(xw + 31, rs.n * g - 1);
     const bool any = xw < rs.n * g;
-    all_end = rs.p0 + xw / g + 1;
-    wend = any ? rs.p0 + last / g + 1 : 0;
+    all_end = rs.p0 + uniform(xw / g) + 1;
+    wend = any ? rs.p0 + uniform(last / g) + 1 : 0;
     all_lo = any ? window_start(wend - 1, a.window) : 0;
     wlo = window_start(all_end - 1, a.window);
   }
@@ -578,12 +583,14 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     __syncthreads();
     const int end = imax(imax(bounds[0][1], bounds[1][1]), imax(bounds[2][1], bounds[3][1]));
     const int lo = imin(imin(bounds[0][0], bounds[1][0]), imin(bounds[2][0], bounds[3][0]));
-    kb.set(0, a.sinks, __builtin_amdgcn_readfirstlane(imin(lo, end)), __builtin_amdgcn_readfirstlane(end));
+    kb.set(0, a.sinks, uniform(imin(lo, end)), uniform(end));
   } else {
     const int last = imin(x0 + kTileCols - 1, rs.n * g - 1);
-    kb.set(0, a.sinks, window_start(rs.p0 + x0 / g, a.window), rs.p0 + last / g + 1);
+    kb.set(0, a.sinks, window_start(rs.p0 + uniform(x0 / g), a.window), rs.p0 + uniform(last / g) + 1);
   }
-  const int i0 = (int)((int64_t)kb.count * split / splits), i1 = (int)((int64_t)kb.count * (split + 1) / splits);
+  // (counts below 2^19, at most 64 splits)
+  const int i0 = uniform((uint32_t)(kb.count * split) / (uint32_t)splits);
+  const int i1 = uniform((uint32_t)(kb.count * (split + 1)) / (uint32_t)splits);
   const int ntile = i1 - i0;
 
   // Blocks [64 c, 64 c + 64) of this split: lane i holds the flags of block 64 c + i and
