@@ -52,4 +52,13 @@ __device__ __forceinline__ float fp4_value(uint32_t code, float scale) {
   return ((code & 8u) ? -v : v) * scale;
 }
 
+// Eight codes (a word, the lowest first) times a scale, as bf16.
+__device__ __forceinline__ bf16x8 fp4_to_bf16(uint32_t w, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
 }  // namespace sr

@@ -24,7 +24,11 @@ template <> __device__ __forceinline__ bf16_t round_once<bf16_t>(double v) {
 // ------------------------------------------------------------------ append
 // A work-group takes one token; a thread takes units of 8 dimensions of a head,
 // HD / 8 neighbouring lanes a head: four rotated pairs, or 8 dimensions that pass.
-// Everything in 64 bits, rounded once.
+// Everything in 64 bits, rounded once.  Memory bounds it: 19 ragged prompts of up to 2333
+// tokens, 48 heads of 64 dimensions, into 4 bits 134 us (with the read below 697 MB in 154,
+// 4.5 TB/s, a copy reaches 4.9).  128 threads where a token has up to 512 units, so that
+// few idle in the last pass over it (those prompts, of 384 units: 256 threads 150 us), 256
+// where it has more (512 tokens of 768 units: 9 us with 256, 13 with 128).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) append_norm_kernel(PageAppendNormArgs na) {
   constexpr int UPH = HD / 8, NG = HD / 32;   // units of a head, groups of 4-bit values
@@ -36,13 +40,13 @@ __global__ void __launch_bounds__(256) append_norm_kernel(PageAppendNormArgs na)
   const int n = clamp_new(a.n_new ? a.n_new[row] : a.lr, a.lr, len);
   if (t >= n) return;
   const int pos = len - n + t, pairs = a.rot >> 1;
-  for (int i = threadIdx.x; i < pairs; i += 256) sincos((double)pos * a.freqs[i], &sn[i], &cs[i]);
+  for (int i = threadIdx.x; i < pairs; i += blockDim.x) sincos((double)pos * a.freqs[i], &sn[i], &cs[i]);
   __syncthreads();
   const int pg = a.table[(int64_t)row * a.max_pages + (pos >> a.shift)];
   const int heads = a.hq + 2 * a.hkv;
   const float* src = a.qkv + (int64_t)blockIdx.x * heads * HD;
   float* qd = a.q + (int64_t)blockIdx.x * a.hq * HD;
-  for (int u = threadIdx.x; u < heads * UPH; u += 256) {   // (the lanes of a head stay together)
+  for (int u = threadIdx.x; u < heads * UPH; u += blockDim.x) {   // (the lanes of a head stay together)
     const int h = u / UPH, w = u % UPH;
     const bool rotates = 4 * w < pairs && h < a.hq + a.hkv;
     // the unit's two runs of four dimensions
@@ -128,22 +132,27 @@ __global__ void __launch_bounds__(256) append_norm_kernel(PageAppendNormArgs na)
     } else {
       if (!is_page(pg, a.n_pages)) continue;
       T* dst = (T*)pool + page_offset(pg, a.hkv, kh, a.shift, pos, HD);
+      typedef T t4 __attribute__((ext_vector_type(4)));   // (multiples of four: aligned)
+      t4 x0, x1;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        dst[d0 + e] = round_once<T>(v0[e]);
-        dst[d1 + e] = round_once<T>(v1[e]);
+        x0[e] = round_once<T>(v0[e]);
+        x1[e] = round_once<T>(v1[e]);
       }
+      *reinterpret_cast<t4*>(dst + d0) = x0;
+      *reinterpret_cast<t4*>(dst + d1) = x1;
     }
   }
 }
 
 template <typename T>
 static void append_norm_by_hd(const PageAppendNormArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.a.rows * a.a.lr));
+  const int units = (a.a.hq + 2 * a.a.hkv) * (a.a.hd / 8);
+  const dim3 grid((unsigned)(a.a.rows * a.a.lr)), block(units <= 512 ? 128 : 256);
   switch (a.a.hd) {
-    case 32: SR_LAUNCH((append_norm_kernel<T, 32>), grid, dim3(256), 0, s, a); break;
-    case 64: SR_LAUNCH((append_norm_kernel<T, 64>), grid, dim3(256), 0, s, a); break;
-    default: SR_LAUNCH((append_norm_kernel<T, 128>), grid, dim3(256), 0, s, a); break;
+    case 32: SR_LAUNCH((append_norm_kernel<T, 32>), grid, block, 0, s, a); break;
+    case 64: SR_LAUNCH((append_norm_kernel<T, 64>), grid, block, 0, s, a); break;
+    default: SR_LAUNCH((append_norm_kernel<T, 128>), grid, block, 0, s, a); break;
   }
   SR_CHECK_LAUNCH();
 }
@@ -156,40 +165,37 @@ void page_append_norm(const PageAppendNormArgs& a, hipStream_t s) {
 }
 
 // -------------------------------------------------------------------- read
-// A thread takes 8 dimensions of a key or value.
-template <typename C, typename T>
-__global__ void __launch_bounds__(256) read_kernel(PageReadArgs a) {
-  const int uph = a.hd / 8;
-  const int64_t units = (int64_t)a.rows * a.lr * a.hkv * uph;
-  const bool value = blockIdx.y != 0;
-  const void* pool = value ? a.vpool : a.kpool;
-  T* out = (T*)(value ? a.v_out : a.k_out);
-  if (!out) return;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
-    const int w = (int)(i % uph), h = (int)(i / uph % a.hkv);
-    const int token = (int)(i / ((int64_t)uph * a.hkv));
-    const int row = token / a.lr, t = token - row * a.lr;
-    const int len = clamp_len(a.lens[row], a.max_pages, a.shift);
-    const int n = clamp_new(a.n_new ? a.n_new[row] : a.lr, a.lr, len);
-    if (t >= n) continue;
-    const int pos = len - n + t;
-    const int pg = a.table[(int64_t)row * a.max_pages + (pos >> a.shift)];
+// A thread takes 8 dimensions of a key and of a value; a work-group whole tokens, as many
+// as fill it.  Those prompts' 8 heads out of 4 bits: 22 us (work-groups of 256 units of keys
+// or of values, each unit's token by a 64-bit division: 39).
+constexpr int kReadThreads = 256;
+template <typename C, typename T, int HD>
+__device__ __forceinline__ void read_unit(const PageReadArgs& a, const void* pool, int pg, int h, int pos, int w, T* dst) {
+  if constexpr (sizeof(C) == 1) {
+    uint32_t c = 0;
+    float scale = 1.f;
+    if (is_page(pg, a.n_pages)) {
+      const int slot = pos & ((1 << a.shift) - 1);
+      const uint8_t* blk = (const uint8_t*)pool + fp4_block(pg, a.hkv, h, a.shift, HD);
+      c = *reinterpret_cast<const uint32_t*>(blk + fp4_codes(slot, HD) + 4 * w);
+      scale = fp4_scale(blk[fp4_scales(slot, a.shift, HD) + w / 4]);
+    }
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x8*>(dst) = fp4_to_bf16(c, scale);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fp4_value(c >> (4 * e), scale);
+      reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (is_page(pg, a.n_pages)) {
-      if constexpr (sizeof(C) == 1) {
-        const int slot = pos & ((1 << a.shift) - 1);
-        const uint8_t* blk = (const uint8_t*)pool + fp4_block(pg, a.hkv, h, a.shift, a.hd);
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(blk + fp4_codes(slot, a.hd) + 4 * w);
-        const float s = fp4_scale(blk[fp4_scales(slot, a.shift, a.hd) + w / 4]);
+      const C* src = (const C*)pool + page_offset(pg, a.hkv, h, a.shift, pos, HD) + 8 * w;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fp4_value(c >> (4 * e), s);
-      } else {
-        const C* src = (const C*)pool + page_offset(pg, a.hkv, h, a.shift, pos, a.hd) + 8 * w;
-#pragma unroll
-        for (int e = 0; e < 8; e += Vec16<C>::N) Vec16<C>::load(src + e, v + e);
-      }
+      for (int e = 0; e < 8; e += Vec16<C>::N) Vec16<C>::load(src + e, v + e);
     }
-    T* dst = out + 8 * i;
     if constexpr (sizeof(T) == 2) {
       uint32_t p[4];
 #pragma unroll
@@ -202,20 +208,52 @@ __global__ void __launch_bounds__(256) read_kernel(PageReadArgs a) {
   }
 }
 
-template <typename C>
+__host__ __device__ inline int read_tokens(int units) { return units < kReadThreads ? kReadThreads / units : 1; }   // of a work-group
+
+template <typename C, typename T, int HD>
+__global__ void __launch_bounds__(kReadThreads) read_kernel(PageReadArgs a) {
+  constexpr int UPH = HD / 8;
+  const int units = a.hkv * UPH, per = read_tokens(units);
+  const int mine = per > 1 ? (int)threadIdx.x / units : 0;
+  const int token = blockIdx.x * per + mine;
+  if (mine >= per || token >= a.rows * a.lr) return;
+  const int row = token / a.lr, t = token - row * a.lr;
+  const int len = clamp_len(a.lens[row], a.max_pages, a.shift);
+  const int n = clamp_new(a.n_new ? a.n_new[row] : a.lr, a.lr, len);
+  if (t >= n) return;
+  const int pos = len - n + t;
+  const int pg = a.table[(int64_t)row * a.max_pages + (pos >> a.shift)];
+  for (int u = threadIdx.x - mine * units; u < units; u += kReadThreads) {   // (once where it holds several tokens)
+    const int h = u / UPH, w = u % UPH;
+    const int64_t at = ((int64_t)token * units + u) * 8;
+    if (a.k_out) read_unit<C, T, HD>(a, a.kpool, pg, h, pos, w, (T*)a.k_out + at);
+    if (a.v_out) read_unit<C, T, HD>(a, a.vpool, pg, h, pos, w, (T*)a.v_out + at);
+  }
+}
+
+template <typename C, typename T>
 static void launch_read(const PageReadArgs& a, hipStream_t s) {
-  const int64_t units = (int64_t)a.rows * a.lr * a.hkv * (a.hd / 8);
-  const dim3 grid((unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16), 2);
-  if (a.dtype == SR_BF16) SR_LAUNCH((read_kernel<C, bf16_t>), grid, dim3(256), 0, s, a);
-  else SR_LAUNCH((read_kernel<C, float>), grid, dim3(256), 0, s, a);
+  const int per = read_tokens(a.hkv * (a.hd / 8));
+  const dim3 grid((unsigned)((a.rows * a.lr + per - 1) / per)), block(kReadThreads);
+  switch (a.hd) {
+    case 32: SR_LAUNCH((read_kernel<C, T, 32>), grid, block, 0, s, a); break;
+    case 64: SR_LAUNCH((read_kernel<C, T, 64>), grid, block, 0, s, a); break;
+    default: SR_LAUNCH((read_kernel<C, T, 128>), grid, block, 0, s, a); break;
+  }
   SR_CHECK_LAUNCH();
+}
+
+template <typename C>
+static void read_by_type(const PageReadArgs& a, hipStream_t s) {
+  if (a.dtype == SR_BF16) launch_read<C, bf16_t>(a, s);
+  else launch_read<C, float>(a, s);
 }
 
 void page_read(const PageReadArgs& a, hipStream_t s) {
   if (a.rows <= 0 || a.lr <= 0) return;
-  if (a.cache == SR_FP4) launch_read<uint8_t>(a, s);
-  else if (a.cache == SR_BF16) launch_read<bf16_t>(a, s);
-  else launch_read<float>(a, s);
+  if (a.cache == SR_FP4) read_by_type<uint8_t>(a, s);
+  else if (a.cache == SR_BF16) read_by_type<bf16_t>(a, s);
+  else read_by_type<float>(a, s);
 }
 
 }  // namespace sr
