@@ -122,6 +122,9 @@ __device__ __forceinline__ __bf16 my_part(float x, int part) {
 // run of 64.  The keys below common[row] are another pass's.  Keys that nobody sees are
 // read where they lie (their scores are masked) and their values as zeros; a half
 // without a page is read from page 0.
+// Memory bounds long rows: 5 of 30-60k keys, 8 heads of 128 dimensions, 245 MB in 44 us
+// (5.6 TB/s; a kernel that only reads reaches 5.5 to 6), the merge 5.5 us behind it.  512
+// rows' own 41 to 460 keys 36 us (every wave has its own start and merge).
 template <int HD, int NW, bool F32, int SPREAD>
 __global__ void __launch_bounds__(64 * NW, HD == 128 && SPREAD == 1 ? 3 : 4)
 fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
@@ -470,17 +473,22 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 //                 32x32x64 on their codes and scale bytes, times queries in three parts of
 //                 6 bits (e2m3), each with a scale for 32 dimensions: 2^-14 of the
 //                 largest of these is left, and products are cut at some 2^-14 of a
-//                 group's largest.  6011 tokens, hd 128: 323 us, 917 TFLOP/s; queries in
-//                 one bf16 341 us and with twice the error, in two 537 us.  53 chunks of
-//                 up to 333 tokens, hd 64: 150, 134 and 166 us.
-// What bounds it: a block of 32 x 32 scores is 256 clocks of exponentials and some 250
-// of other vector work a wave, beside 512 (hd 128) of matrix work.  Lane i keeps the place and the mask flags of block i of a run of 64.
+//                 group's largest.  6011 tokens, hd 128: 323 us; queries in one bf16 341
+//                 us and half as precise, in two 537 us.  53 chunks of up to 333 tokens,
+//                 hd 64: 150, 134 and 166 us.
+//                 The maximum is taken off by one more product, not by vector work
+//                 (200 tokens on 60k keys 229 -> 209 us).
+// With lengths and block numbers in scalar registers 311 and 133 us, with the maximum in
+// the product 307 (965 TFLOP/s) and 131.  What bounds it: a block of 32 x 32 scores is 256
+// clocks of exponentials and some 250 of other vector work a wave, beside 480 (hd 128) or
+// 256 of matrix work, and the waves of a SIMD hardly overlap them.  The next block's
+// scores beneath this one's exponentials, or two blocks a barrier: the same time.  Lane i keeps the place and the mask flags of block i of a run of 64.
 // The output is rescaled only when a maximum has moved by more than
 // kStale.
 constexpr int kTileCols = 128;
 
 template <int HD, bool PRE, bool F32>
-__global__ void __launch_bounds__(256, HD == 128 || PRE || F32 ? 2 : 3)
+__global__ void __launch_bounds__(256, HD == 128 || PRE || F32 ? 2 : 4)
 fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int slots, float qscale) {
   constexpr int KT = 32, NW = 4;
   constexpr int KS = HD / 16, DT = HD / 32, CPK = HD / 8;
@@ -716,7 +724,13 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   // probabilities are exp2(-inf) = 0, where -inf - -inf would be NaN; for columns
   // that are no query from +inf, which no score of theirs passes, so that they
   // never rescale the others
-  float m = live ? -FLT_MAX : INFINITY, l = 0.f;
+  // CODES: scores come out of the products less the maximum so far (0 at first), which
+  // enters as three bf16 parts (all 24 bits) times ones; `limit` is what they may reach
+  // until it moves: anything finite before a column's first score
+  float m = CODES ? 0.f : live ? -FLT_MAX : INFINITY, l = 0.f;
+  float limit = live ? -FLT_MAX : INFINITY;
+  bf16x8 less = {}, ones3 = {};
+  ones3[0] = ones3[1] = ones3[2] = (__bf16)(fh == 0 ? 1.f : 0.f);
 
   auto frag = [&](const bf16_t* base, int s) {
     return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(base) + (kbase ^ (32u * s)));
@@ -731,6 +745,7 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
       // key fr's codes, and the scale bytes from the lane's first group on (32 dimensions:
       // the queries are 0 in the other half, where the codes stand in for themselves)
       const uint32_t ks = *reinterpret_cast<const uint32_t*>(raw_scale[ST] + 4 * fr) >> (HD == 32 ? 0 : 8 * fh);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones3, less, sc, 0, 0, 0);
       i32x8 k[LJ];
 #pragma unroll
       for (int j = 0; j < LJ; ++j) {
@@ -773,12 +788,21 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 #pragma unroll
     for (int e = 1; e < 16; ++e) mt = fmaxf(mt, sc[e]);
     mt = fmaxf(mt, other_half(mt));
-    if (__any(mt > m + kStale)) {
-      const float mn = fmaxf(m, mt);
-      const float corr = __builtin_amdgcn_exp2f(m - mn);
+    if (CODES ? __any(mt > limit) : __any(mt > m + kStale)) {
+      const bool moves = mt > limit;
+      const float mn = CODES ? (moves ? m + mt : m) : fmaxf(m, mt);
+      const float corr = CODES && limit != kStale ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= corr;
+      if constexpr (CODES) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] -= mn - m;
+        __bf16 p[3];
+        in_parts<3>(fh == 0 ? -mn : 0.f, p);
+        less[0] = p[0]; less[1] = p[1]; less[2] = p[2];
+        if (moves) limit = kStale;
+      }
       m = mn;
     }
     uint32_t va[DT];
@@ -790,7 +814,7 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float pv = __builtin_amdgcn_exp2f(sc[8 * c + e] - m);
+        const float pv = __builtin_amdgcn_exp2f(CODES ? sc[8 * c + e] : sc[8 * c + e] - m);
         __bf16 p[PP];
         in_parts<PP>(pv, p);
 #pragma unroll
@@ -903,6 +927,7 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
   l += other_half(l);
   if (PRE || slots > 1) {
     if (!live) return;
+    if (CODES && limit != kStale) m = -FLT_MAX;   // (nothing seen: below every other part's)
     const Partials pt{a.part, (int64_t)a.rows * a.lr * a.hq, slots};
     const int x = xw + fr, tok = x / g;
     const int64_t th = (int64_t)(token0 + tok) * a.hq + h * g + (x - tok * g);

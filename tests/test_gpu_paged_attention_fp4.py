@@ -177,6 +177,28 @@ def test_what_queries_keep_beyond_a_bf16(hd, hq, hkv, lr):
     assert np.linalg.norm(out - ref) / size <= np.hypot(lost / 4, np.sqrt(2) * 2.0 ** -9)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_scores_far_from_zero(bf16, hd, hq, hkv, sign):
+    """All scores of a row some hundreds below or above 0; a window leaves whole splits
+    and blocks unseen."""
+    torch, sr = need_gpu()
+    say(f"attention over 4 bits, far scores bf16={bf16} hd={hd} sign={sign}")
+    rng = np.random.default_rng(hd + sign)
+    lens = [700, 75, 1]
+    for lr, window, sinks in ((1, 0, 0), (40, 0, 0), (40, 70, 3), (1, 5, 1)):
+        cache = Cache4(rng, lens, 32, hkv, hd)
+        cache.raw[0] = (cache.raw[0][0] & 7, np.full_like(cache.raw[0][1], 126))      # all positive, of one scale
+        cache.k = dequantise(*cache.raw[0])
+        new = new_tokens(lens, [lr] * 3, lr)
+        cache.poison(new, window, sinks)
+        q = (sign * 40 * (1 + 0.02 * rng.normal(size=(3, lr, hq, hd)))).astype(np.float32)
+        out, _ = run(torch, sr, cache, q, [lr] * 3, bf16, window, sinks)
+        ref, bound = attention(cache, q, new, window, sinks, bf16)
+        check(out, ref, bound, new)
+
+
 def test_pools_past_32_bits():
     """Pages that lie past 2^32 bytes of a pool hold what is put there, and are read
     from there: as a small pool of the same tokens, bit for bit."""
