@@ -141,3 +141,53 @@ def test_candidates_in_four_bits(bf16, hd, window, sinks, pt):
         sr.page_reserve(pool, table, lens, refs, 1, table, lens, refs, granted, info)
         assert info.tolist()[:2] == [0, 0] and granted.tolist() == [1] * N
         logits = forward(tok.view(N, 1), table, lens, granted, P // pt * pt)
+
+
+def test_two_graphs_over_one_memory_pool():
+    """Two captured steps whose workspaces share memory, replayed in turn with eager
+    calls between them: the results of the eager calls, bit for bit."""
+    torch, sr = need_gpu()
+    say("two graphs over one memory pool")
+    hd, hq, hkv, pt, vocab = 64, 8, 2, 64, 50001
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    steps = []
+    for rows, length in ((3, 5000), (7, 900)):
+        mp = -(-length // pt)
+        table = torch.randperm(rows * mp, device="cuda", generator=gen).to(torch.int32).view(rows, mp)
+        lens = torch.full((rows,), length, dtype=torch.int32, device="cuda") - torch.arange(rows, dtype=torch.int32, device="cuda")
+        k, v = (torch.zeros((rows * mp, hkv, pt, sr.fp4_token_bytes(hd)), dtype=torch.uint8, device="cuda") for _ in range(2))
+        fill = torch.zeros((rows, length, hq, hd), device="cuda")
+        sr.page_append_norm(rnd(rows, length, (hq + 2 * hkv) * hd), None, table, lens, k, v, fill, n_new=lens)
+        qkv, head, words = rnd(rows, 1, (hq + 2 * hkv) * hd), rnd(vocab, hq * hd) / 10, torch.arange(rows, dtype=torch.int32, device="cuda") * 98765431
+        q = torch.zeros((rows, 1, hq, hd), device="cuda")
+        o, logits = torch.zeros((rows, 1, hq * hd), device="cuda"), torch.zeros((rows, vocab), device="cuda")
+        tok, lp, kept = torch.zeros_like(lens), torch.zeros(rows, device="cuda"), torch.zeros_like(lens)
+
+        def step(a=(qkv, table, lens, k, v, q, o, logits, head, words, tok, lp, kept)):
+            qkv, table, lens, k, v, q, o, logits, head, words, tok, lp, kept = a
+            sr.page_append_norm(qkv, None, table, lens, k, v, q)          # (the last token again)
+            sr.paged_attention_fp4(q, k, v, table, lens, o)
+            sr.projection(o.view(len(lens), -1), head, 0, logits)
+            sr.sample_filtered(logits, words, tok, top_k=50, top_p=0.9, logprob=lp, kept=kept)
+            return o, tok, lp, kept
+        steps.append(step)
+    want = [[t.clone() for t in s()] for s in steps]
+    torch.cuda.synchronize()
+    pool, graphs = torch.cuda.graph_pool_handle(), []
+    for s in steps:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], pool=pool):
+            outs = s()
+        steps[len(graphs) - 1] = (s, outs)
+    for i in (0, 1, 0, 0, 1, 1, 0):
+        for _, outs in steps:
+            for t in outs:
+                t.zero_()
+        torch.cuda.synchronize()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(steps[i][1], want[i])), i
+        steps[1 - i][0]()                                               # (eager, with a workspace of its own)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(steps[1 - i][1], want[1 - i])), i
