@@ -16,11 +16,11 @@
 //
 // Measured with fp32 logits of 128256 entries: one row 18 us (its readings by 32
 // work-groups; by one alone 50); 512 rows, of which one half keeps 50 and the rest follow
-// other settings, 115 us, all with a top-k of 50 60 us, with a top-p of 0.9 158 us
+// other settings, 115 us, all with a top-k of 50 60 us, with a top-p of 0.9 154 us
 // (263 MB, 48 us at the rate of a pure read: a second reading, and the exponentials of
-// 66 M entries), unfiltered 114 us.  256 flat rows of 32000 bf16 logits under a top-p of
-// 0.95 58 us: maximum 6, whether a list can be enough 3, bins 15 (64-bit adds in LDS), the
-// border's bin and the sums before it 17 (their exponentials), search 12, drawn entry 4.
+// 66 M entries), unfiltered 104 us.  256 flat rows of 32000 bf16 logits under a top-p of
+// 0.95 53 us: maximum 6, whether a list can be enough 3, bins 15 (64-bit adds in LDS), the
+// border's bin and the sums before it 12 (their exponentials), search 12, drawn entry 4.
 //
 //   filtered_kernel         a work-group of 16 waves a row, from the logits to the token
 //   filtered_maxima_kernel, few rows: the two readings by work-groups of four tiles
@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
   // f(four neighbouring values, the first's index), the next ones' loads in flight: for
   // the passes of rows that no list decides, where fetching the code of a tile's 16
   // entries takes longer than running it (flat rows under a top-p of 0.95, 16 entries at a
-  // time -> 4: 256 of 32000 bf16 values 66 -> 57.5 us, 512 of 128256 290 -> 222 us).
+  // time -> 4: 256 of 32000 bf16 values 66 -> 57.5 us, 512 of 128256 290 -> 222 us; whole tiles a
+  // wave, so that a tile is summed once: 53 and 203 us).
   auto pass4 = [&](auto&& f) {
     auto load = [&](int i, float (&v)[4]) {
       if (VEC && i + 4 <= vocab) {
@@ -393,15 +394,16 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = seen(v[e]);
     };
-    constexpr int step = 4 * kFltThreads;
+    // quarters of the wave's tiles, one after the other
+    auto at = [&](int j) { return (wave + kFltWaves * (j >> 2)) * kLpTile + 256 * (j & 3) + 4 * lane; };
     float v[4], n1[4], n2[4];
-    int i = 4 * tid;
-    load(i, v);
-    load(i + step, n1);
+    load(at(0), v);
+    load(at(1), n1);
+    const int tiles = (vocab + kLpTile - 1) / kLpTile, count = 4 * ((tiles - wave + kFltWaves - 1) / kFltWaves);
 #pragma unroll 1
-    for (; i < (vocab + 255 & ~255); i += step) {   // (a wave's 256 entries together)
-      load(i + 2 * step, n2);
-      f(v, i);
+    for (int j = 0; j < count; ++j) {
+      load(at(j + 2), n2);
+      f(v, at(j));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         v[e] = n1[e];
@@ -651,6 +653,7 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
       kept = 0;
       __syncthreads();
       const float near = (float)b, far = (float)(b + 1);
+      uint64_t sum = 0;   // of this lane, in its tile
       pass4([&](const float(&v)[4], int i) {
         uint32_t in = 0, before = 0;
 #pragma unroll
@@ -661,12 +664,21 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
           in |= (uint32_t)(here && !out) << e;
           before |= (uint32_t)(p < near) << e;
         }
-        if (last && __any(before != 0)) {
-          uint64_t w = rd.weights(v, [&](int e, uint32_t u) { return (before >> e & 1) && u >= rd.least; });
-#pragma unroll
-          for (int e = 0; e < 4; ++e) kept += (before >> e & 1) && rd.weight_word(v[e]) >= max(rd.least, 1u);
-          w = wave_scan64(w);
-          if (lane == 63) atomicAdd((unsigned long long*)&sh.tile[i / kLpTile], (unsigned long long)w);
+        if (last) {
+          if (__any(before != 0)) {
+            uint32_t mine = 0;
+            sum += rd.weights(v, [&](int e, uint32_t u) {
+              const bool in = (before >> e & 1) && u >= rd.least;
+              mine |= (uint32_t)(in && u != 0) << e;
+              return in;
+            });
+            kept += __popc(mine);
+          }
+          if ((i & 1023) >= 768) {   // (uniform: the tile's last quarter)
+            const uint64_t w = wave_scan64(sum);
+            if (lane == 63) sh.tile[i / kLpTile] = w;
+            sum = 0;
+          }
         }
         if (!__any(in != 0)) return;
         const uint32_t mine = __popc(in), upto = wave_scan32(mine);
