@@ -10,9 +10,11 @@
 //
 // Two codes and their scale become two bf16 in one instruction, exactly
 // (v_cvt_scalef32_pk_bf16_fp4), so the products see the cache's own values, and what
-// is rounded is the queries and the probabilities.  They enter as QP and PP parts of
-// 8 bits each: what a rounding to bf16 leaves is the next part, and the products add
-// up.  Outputs in fp32 take three parts of either, all 24 bits.
+// is rounded is the queries and the probabilities.  They enter as parts of 8 bits each:
+// what a rounding to bf16 leaves is the next part, and the products add up.  Outputs in
+// fp32 take three parts of either, all 24 bits; in bf16 two of a query and one of a
+// probability; prompts in bf16 multiply the codes themselves with queries in parts of 6
+// bits (fp4_tile_kernel).
 // Online softmax in base 2 (queries carry log2 e / sqrt(head_dim)).  A score that is
 // NaN never raises a maximum and always enters the sum, so "nothing seen" is a sum
 // equal to 0 and a maximum of -inf says nothing about the sum.
