@@ -46,6 +46,7 @@ constexpr int kPLanes = 50;        // lanes of a wave whose maxima the list for 
 constexpr int kFltTiles = 256;     // of a row (262144 entries)
 constexpr int kFltSplitWaves = 4;  // tiles of a work-group of the split readings
 constexpr int kFltMaxima = 64 * kFltTiles / kFltSplitWaves;   // of a row, of the split readings
+constexpr float kMasked = -3.38e38f;   // above the lowest values of fp32 and bf16, which mask entries
 
 // Work-groups of a row of the split readings.
 __host__ __device__ inline int split_chunks(int vocab) {
@@ -70,6 +71,10 @@ struct FilteredShared {
   int n, c, bin;
 };
 
+// What all lanes hold alike, told to the compiler: it then stays in a scalar register.
+__device__ __forceinline__ float uniform(float v) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
 __device__ __forceinline__ float seen(float x) { return fmaxf(x, -INFINITY); }   // NaN counts as -inf
 // A row whose maximum is +inf is read as 0 there and -inf elsewhere.
 template <int N>
@@ -422,12 +427,12 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
     if (a.kept) a.kept[r] = kept;
   };
 
-  // Lists those of a tile that reach `from`: one reservation a wave, its lanes' entries
+  // Lists those of a tile that `wanted` holds for: one reservation a wave, its lanes' entries
   // one lane after the other.
-  auto list_from = [&](const float(&v)[16], int base, float from) {
+  auto list_those = [&](const float(&v)[16], int base, auto&& wanted) {
     uint32_t in = 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) in |= (uint32_t)(v[e] >= from) << e;
+    for (int e = 0; e < 16; ++e) in |= (uint32_t)wanted(v[e]) << e;
     if (!__any(in != 0)) return;
     const uint32_t mine = __popc(in), upto = wave_scan32(mine);
     int at = 0;
@@ -458,14 +463,18 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
   };
 
   // The maximum.  Under a top-k of a long row, every wave also lists what reaches a bound
-  // that it takes from its first tile: if the k-th of the listed reaches the highest of
-  // these bounds, the list holds the first k.  Else a value that at least k entries
-  // reach is the least of the waves' k / waves-th largest lanes' maxima (of those that have
-  // a whole tile), and another pass lists them.
+  // that it takes from its first tile (from its later ones while they hold hardly more than
+  // masks): if the k-th of the listed reaches the highest of these bounds, the list holds
+  // the first k.  Else at least k entries reach that k-th, and the waves whose bounds are
+  // above it list what lies between (logits that fall with the index, 512 x 128256, top-k
+  // 50: 72 us, 62 where they do not; by bins 149).  Without k listed, or with too many, a
+  // value that at least k entries reach is the least of the waves' k / waves-th largest
+  // lanes' maxima (of those that have a whole tile), and another pass lists them (so it does
+  // for top-p alone).
   const int whole = min(kFltWaves, vocab / kLpTile);
   const bool by_list = (rd.by_k && (rd.k <= 64 * whole || vocab <= kFltList)) || (!rd.by_k && rd.by_p);
   const bool at_once = !SPLIT && rd.by_k && !rd.greedy && rd.k <= kFltThreads && vocab >= 2 * kFltWaves * kLpTile;
-  float from = -FLT_MAX, highest = -FLT_MAX;
+  float from = -FLT_MAX, highest = -FLT_MAX, own = kMasked;   // (own: of the wave)
   if (tid == 0) sh.n = 0;
   __syncthreads();
   {
@@ -474,16 +483,15 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
     if constexpr (SPLIT) {
       for (int i = tid; i < split_chunks(vocab) * 64; i += kFltThreads) mt = fmaxf(mt, given->maxima[i]);
     } else {
-      float own = INFINITY;
       pass([&](const float(&v)[16], int base) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) mt = fmaxf(mt, v[e]);
         if (at_once) {
-          if (base == wave * kLpTile) {
+          if (own == kMasked) {   // (uniform)
             first = reached(key_of(mt), min(64, 8 + (int)(2 * (int64_t)rd.k * kLpTile / vocab)));
-            own = value_of(first);
+            own = uniform(fmaxf(value_of(first), kMasked));
           }
-          list_from(v, base, own);
+          list_those(v, base, [&](float l) { return l >= own; });
         }
       });
       if (wave < whole) bound = reached(key_of(mt), rd.by_k ? (rd.k + whole - 1) / whole : kPLanes);
@@ -496,8 +504,8 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
     __syncthreads();
     const uint64_t w = lane < kFltWaves ? sh.wave[lane] : 0;
     rd.m = word_value((uint64_t)wave_max_u32((uint32_t)(w >> 32)) << 32);
-    if (vocab > kFltList) from = value_of(~wave_max_u32((uint32_t)w));
-    highest = value_of(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0));
+    if (vocab > kFltList) from = uniform(value_of(~wave_max_u32((uint32_t)w)));
+    highest = uniform(value_of(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0)));
   }
   if (rd.m == -INFINITY) {
     if (tid == 0) answer(0, -INFINITY, 0);
@@ -552,32 +560,50 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
     flat = (float)(uint32_t)(sums >> 32) < 0.9f * (float)(uint32_t)sums * a.top_p[r];
   }
 
-  // The list of the best, where it can be enough.
-  if (by_list && !flat) {
+  // The list of the best, where it can be enough: that of the first pass, or ...
+  float lo = from, hi = INFINITY;   // (another pass lists from lo on, below hi, ...)
+  bool again = true;                // (... from the start, not beside what is listed)
+  if (at_once && !infinite) {
+    const int n = sh.n;
+    if (n <= kFltList && n >= rd.k) {
+      const ListCut c = cut_list(sh, rd, n, BY_K | (rd.by_p ? BY_P : 0) | BY_INDEX, (uint64_t)rd.k, 0, 0, 0.f, 1.f, word, highest);
+      if (c.found) {
+        draw(c);
+        return;
+      }
+      lo = fmaxf(lo, uniform(word_value(c.border)));
+      hi = own;
+      again = false;
+    }
+  }
+  // ... of another one.  (For a top-k near the number of lanes that would take in too many:
+  // 6800 to 8800 entries for 1000 of 128256 in no order, 2300 to 3300 for 896.)
+  if (by_list && !flat && (!at_once || infinite || rd.k <= kFltThreads * 7 / 8)) {
     int n;
     uint64_t total = 0;
-    float end = 0.f;
+    float end = (float)(kFltBins - 1);
     if constexpr (SPLIT) {
       n = (int)given->n;
       total = given->total;
+      end = 0.f;
       if (n <= kFltList)
         for (int i = tid; i < n; i += kFltThreads) {
           sh.list[i] = given->list[i];
           end = fmaxf(end, rd.place(word_value(sh.list[i])));
         }
-    } else if (at_once && !infinite) {
-      n = sh.n;
-      end = (float)(kFltBins - 1);
     } else {
       const bool weigh = !rd.by_k;
-      end = rd.place(from);
       __syncthreads();
-      if (tid == 0) sh.n = 0;
-      __syncthreads();
-      pass([&](const float(&v)[16], int base) {
-        if (weigh) total += rd.weights(v, [](int, uint32_t) { return true; });
-        list_from(v, base, from);
-      });
+      if (again) {
+        end = rd.place(from);
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+      }
+      if (lo < hi)
+        pass([&](const float(&v)[16], int base) {
+          if (weigh) total += rd.weights(v, [](int, uint32_t) { return true; });
+          list_those(v, base, [&](float l) { return (l >= lo) & (l < hi); });
+        });
       total = block_scan(total, sh).all;   // (and every entry is listed)
       n = sh.n;
     }
@@ -589,10 +615,9 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
       end = __uint_as_float(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0));
       __syncthreads();
     }
-    if (n <= kFltList && (!at_once || infinite || n >= rd.k)) {
-      const int searches = (rd.by_k && (at_once || n > rd.k) ? BY_K : 0) | (rd.by_p ? BY_P : 0) | BY_INDEX;
-      const ListCut c = cut_list(sh, rd, n, searches, (uint64_t)rd.k, rd.by_k ? 0 : total, 0, 0.f,
-                                 (float)kFltBins / (end + 1.f), word, at_once && !infinite ? highest : -FLT_MAX);
+    if (n <= kFltList) {
+      const int searches = (rd.by_k && n > rd.k ? BY_K : 0) | (rd.by_p ? BY_P : 0) | BY_INDEX;
+      const ListCut c = cut_list(sh, rd, n, searches, (uint64_t)rd.k, rd.by_k ? 0 : total, 0, 0.f, (float)kFltBins / (end + 1.f), word);
       if (c.found) {
         draw(c);
         return;
