@@ -499,13 +499,13 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
     const uint32_t best = wave_max_u32(key_of(mt));
     if (lane == 0) {
       sh.wave[wave] = (uint64_t)best << 32 | (uint32_t)~bound;
-      sh.wave32[wave] = first;
+      if constexpr (!SPLIT) sh.wave32[wave] = first;
     }
     __syncthreads();
     const uint64_t w = lane < kFltWaves ? sh.wave[lane] : 0;
     rd.m = word_value((uint64_t)wave_max_u32((uint32_t)(w >> 32)) << 32);
     if (vocab > kFltList) from = uniform(value_of(~wave_max_u32((uint32_t)w)));
-    highest = uniform(value_of(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0)));
+    if constexpr (!SPLIT) highest = uniform(value_of(wave_max_u32(lane < kFltWaves ? sh.wave32[lane] : 0)));
   }
   if (rd.m == -INFINITY) {
     if (tid == 0) answer(0, -INFINITY, 0);
