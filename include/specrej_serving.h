@@ -71,8 +71,10 @@ sr_status sr_page_read(int32_t cache, int32_t dtype, int32_t head_dim, int32_t n
  * pages stand for.  out: dtype SR_BF16 or SR_F32.  On the matrix cores, which keys
  * and values enter exactly.  SR_BF16: queries keep 16 bits where a row has at most 16
  * query columns (lr n_heads / n_kv_heads), and where it has more are off by up to 2^-13
- * of the largest of every 32 dimensions; probabilities keep 8 bits; sums are in fp32.  SR_F32: queries and
- * probabilities enter as three parts, all 24 bits.  A layer's keys take less than
+ * of the largest of every 32 dimensions; probabilities keep 16 bits where a row has at
+ * most 8 columns, 8 where it has more and for shared keys that are read once for all
+ * rows; sums are in fp32.  SR_F32: queries and probabilities enter as three parts, all
+ * 24 bits.  A layer's keys take less than
  * 2^36 bytes.  scratch: DEVICE float of scratch_elems >=
  * sr_paged_attention_fp4_scratch(...) elements. */
 sr_status sr_paged_attention_fp4(int32_t dtype, int32_t head_dim, int32_t n_heads, int32_t n_kv_heads,

@@ -12,9 +12,10 @@
 // (v_cvt_scalef32_pk_bf16_fp4), so the products see the cache's own values, and what
 // is rounded is the queries and the probabilities.  They enter as parts of 8 bits each:
 // what a rounding to bf16 leaves is the next part, and the products add up.  Outputs in
-// fp32 take three parts of either, all 24 bits; in bf16 two of a query and one of a
-// probability; prompts in bf16 multiply the codes themselves with queries in parts of 6
-// bits (fp4_tile_kernel).
+// fp32 take three parts of either, all 24 bits; in bf16 two of a query and, where a second
+// one costs no product (up to 8 columns, fp4_wave_kernel), two of a probability, else one;
+// prompts in bf16 multiply the codes themselves with queries in parts of 6 bits
+// (fp4_tile_kernel).
 // Online softmax in base 2 (queries carry log2 e / sqrt(head_dim)).  A score that is
 // NaN never raises a maximum and always enters the sum, so "nothing seen" is a sum
 // equal to 0 and a maximum of -inf says nothing about the sum.
@@ -90,8 +91,11 @@ __device__ __forceinline__ RowState uniform(const RowState& r) { return {uniform
 
 // ------------------------------------------------------- waves split keys
 // Query columns of a work-group and where their parts go: with up to 8 (4) columns each
-// is there SPREAD = 2 (4) times, and the matrix columns hold a part each, at no
-// product more; else every part takes products of its own.
+// is there SPREAD = 2 (4) times, and the matrix columns hold a part each of its query and
+// of its probabilities, at no product more; else every part takes products of its own (of
+// probabilities in bf16 there is one then).  Probabilities in two parts against one: 5
+// rows of 30-60k keys 60 us for 60, outputs 0.0017 (their own rounding) off in the 2-norm
+// for 0.0022; 512 rows on 1024 shared keys 72 us for 71.5.
 template <bool F32, int SPREAD>
 struct Fp4Parts {
   static constexpr int COLS = 16 / SPREAD;
@@ -340,8 +344,9 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     for (int i = 0; i < 8; ++i) {
       float pv = __builtin_amdgcn_exp2f(sv[i] - m);
       ps += pv;
-      if constexpr (F32 && SPREAD > 1) {
-        pf[0][i] = my_part<SPREAD, 3>(pv, part);
+      if constexpr (SPREAD > 1) {
+        if constexpr (F32) pf[0][i] = my_part<SPREAD, 3>(pv, part);
+        else pf[0][i] = (__bf16)(part == 0 ? pv : pv - (float)(__bf16)pv);
       } else {
         __bf16 p[PSETS];
         in_parts<PSETS>(pv, p);
@@ -432,7 +437,15 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
     for (int k = 0; k < NW; ++k) {
       const float* ws = sm + (k * 16 + c) * ROW;
       const f32x4 u = *reinterpret_cast<const f32x4*>(ws + d), v = *reinterpret_cast<const f32x4*>(ws + d + 4);
-      const float o8[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+      float o8[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+      if constexpr (!F32 && SPREAD > 1) {   // (the outputs of the probabilities' second parts)
+        const f32x4 u2 = *reinterpret_cast<const f32x4*>(ws + COLS * ROW + d), v2 = *reinterpret_cast<const f32x4*>(ws + COLS * ROW + d + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o8[e] += u2[e];
+          o8[4 + e] += v2[e];
+        }
+      }
       add(ws[HD], ws[HD + 1], o8);
     }
     if (splits == 1) {
