@@ -486,9 +486,10 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 // barrier a block.
 //   CODES (bf16 outputs of prompts): keys are not converted.  S^T is v_mfma_scale_f32_
 //                 32x32x64 on their codes and scale bytes, times queries in three parts of
-//                 6 bits (e2m3), each with a scale for 32 dimensions: 2^-14 of the
-//                 largest of these is left, and products are cut at some 2^-14 of a
-//                 group's largest.  6011 tokens, hd 128: 323 us; queries in one bf16 341
+//                 6 bits (e2m3), each with a scale for 32 dimensions: at most 1 / 15360
+//                 of the largest of these is left.  The products are exact, and a sum of
+//                 64 of them with scales of any size is off by 2^-21 of the largest at
+//                 most (measured).  6011 tokens, hd 128: 323 us; queries in one bf16 341
 //                 us and half as precise, in two 537 us.  53 chunks of up to 333 tokens,
 //                 hd 64: 150, 134 and 166 us.
 //                 The maximum is taken off by one more product, not by vector work
@@ -889,9 +890,14 @@ fp4_tile_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
             odd[e] = x[2 * e + 1];
           }
           q6[p][j] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+          // It writes while it still reads, which the compiler does not know: the sources stay
+          // alive until it is done, or the result may be put into them.  (At head_dim 32 the third
+          // part went to the third register of `even`: scores of 250 were up to 0.1 off.)
+          asm volatile("" : "+v"(q6[p][j]) : "v"(even), "v"(odd), "v"(scale));
           q6_scale[p / 2] |= (uint32_t)(fine ? byte : 255) << (8 * (2 * (p & 1) + j));   // (255: NaN)
           if (p + 1 == QP) break;
-          const f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q6[p][j], scale);
+          f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q6[p][j], scale);
+          asm volatile("" : "+v"(y) : "v"(q6[p][j]), "v"(scale));   // (likewise)
           top = 0.f;
 #pragma unroll
           for (int e = 0; e < 32; ++e) {

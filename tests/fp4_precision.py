@@ -29,8 +29,8 @@ def limit(cache, q, n_new, window, sinks, columns, p_bits=None):
     rounding that is off by u at most is off by u / sqrt(3) in the mean square.  The
     output's is taken as it falls.  A key's score is off by that of a dimension times |k|
     / sqrt(hd), added over the dimensions: a query keeps 16 bits (2^-16 |q|) for up to 16
-    columns; for more it and the products are off by up to 2^-12 of the largest of 32
-    dimensions.  A probability keeps 16 bits (2^-16) for up to 8 columns, 8 bits (2^-8)
+    columns; for more it is off by up to 1 / 15360 of the largest of 32 dimensions
+    (fp4_util.attention derives it; products of 6 bits with 4-bit keys are exact).  A probability keeps 16 bits (2^-16) for up to 8 columns, 8 bits (2^-8)
     for more, or p_bits.  A weight p that is off by e relative moves an output by e p times
     its value, less the output where the sum of the weights moves with it.  A
     tenth on top: the errors add up over some thousand outputs, not over all there could
@@ -55,7 +55,7 @@ def limit(cache, q, n_new, window, sinks, columns, p_bits=None):
                 o = p @ vs
                 per = 2.0 ** -16 * np.abs(qh)
                 if columns > 16:
-                    per = 2.0 ** -12 * np.repeat(np.abs(qh).reshape(g, -1, 32).max(2), 32, axis=1)
+                    per = np.repeat(np.abs(qh).reshape(g, -1, 32).max(2), 32, axis=1) / 15360
                 e2 = (per ** 2 @ (ks ** 2).T / hd + up ** 2) / 3          # of a weight, squared
                 w2 = p ** 2 * e2
                 moved = np.maximum(w2 @ vs ** 2, w2 @ vs ** 2 - 2 * o * (w2 @ vs) + o ** 2 * w2.sum(1, keepdims=True))

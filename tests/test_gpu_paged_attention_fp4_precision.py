@@ -6,8 +6,8 @@ probability."""
 import numpy as np
 import pytest
 
-from fp4_precision import limit, with_8_bits
-from fp4_util import Cache4
+from fp4_precision import limit, six_bit_parts, with_8_bits
+from fp4_util import Cache4, dequantise
 from gpu_util import need_gpu, say
 from paged_util import new_tokens
 from test_gpu_paged_attention_fp4 import run
@@ -35,3 +35,48 @@ def test_up_to_8_columns_are_off_by_the_outputs_rounding(hd, hq, hkv, lr):
         assert error(with_8_bits(cache, q, new, window, sinks), ref, new) > most    # (or there is nothing to see)
         out, _ = run(torch, sr, cache, q, [lr] * len(lens), True, window, sinks)
         assert error(out, ref, new) <= most, (error(out, ref, new) / np.linalg.norm(ref), most / np.linalg.norm(ref))
+
+
+def in_parts(q, parts):
+    """Queries as the prompts' products see them: parts of 6 bits."""
+    scale = np.float32(1.4426950408889634 / np.sqrt(q.shape[-1]))
+    return six_bit_parts(q * scale, parts)[0] / scale
+
+
+def check_prompt(cache, q, lens, window, sinks, needed, what):
+    """Its 2-norm; that queries of fewer than `needed` parts would exceed the limit is seen
+    first."""
+    rows, lr, hq, hd = q.shape
+    new = new_tokens(lens, [lr] * rows, lr)
+    cache.poison(new, window, sinks)
+    ref, most = limit(cache, q, new, window, sinks, lr * hq // cache.hkv)
+    whole, short = (limit(cache, in_parts(q, n), new, window, sinks, 99)[0] for n in (3, needed - 1))
+    assert error(whole, ref, new) < most / 4 and error(short, ref, new) > most
+    torch, sr = need_gpu()
+    say(f"attention over 4 bits, precision of prompts {what} hd={hd} {hq}/{cache.hkv} lr={lr} window={window}")
+    out, _ = run(torch, sr, cache, q, [lr] * rows, True, window, sinks)
+    assert error(out, ref, new) <= most, (error(out, ref, new) / np.linalg.norm(ref), most / np.linalg.norm(ref))
+
+
+def positive_keys(cache):
+    cache.raw[0] = (cache.raw[0][0] & 7, np.full_like(cache.raw[0][1], 126))      # of one scale
+    cache.k = dequantise(*cache.raw[0])
+
+
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_prompts_whose_far_scores_almost_tie(hd, hq, hkv, sign):
+    """Every token sees two keys whose scores, some hundreds from 0, differ by about 1:
+    every part of a query moves the output."""
+    rng = np.random.default_rng(hd + sign)
+    lens, lr = [200, 131], 70
+    cache = Cache4(rng, lens, 16, hkv, hd)
+    positive_keys(cache)
+    q = sign * 60 * (1 + 0.5 * rng.normal(size=(2, lr, hq, hd)))
+    for r in range(2):
+        k = cache.rows_kv(r)[0]
+        for t in range(lr):
+            pos = lens[r] - lr + t
+            diff = np.repeat(k[pos] - k[pos - 1], hq // hkv, axis=0)
+            q[r, t] += ((rng.normal(size=hq) * np.sqrt(hd) - (q[r, t] * diff).sum(1)) / (diff * diff).sum(1))[:, None] * diff
+    check_prompt(cache, q.astype(np.float32), lens, 2, 0, 3, f"far, close {sign}")
