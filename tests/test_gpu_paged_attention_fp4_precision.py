@@ -64,6 +64,28 @@ def positive_keys(cache):
 
 
 @pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_prompts(hd, hq, hkv, window, sinks):
+    rng = np.random.default_rng(hd)
+    lens = [300, 150, 45]
+    cache = Cache4(rng, lens, 32, hkv, hd)
+    check_prompt(cache, rng.normal(size=(3, 40, hq, hd)).astype(np.float32), lens, window, sinks, 2, "moderate")
+
+
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_prompts_with_scores_far_from_zero(hd, hq, hkv, window, sinks, sign):
+    """All scores of a row some hundreds below or above 0, where the running maximum comes
+    off in the products."""
+    rng = np.random.default_rng(hd + sign)
+    lens = [700, 75, 41]
+    cache = Cache4(rng, lens, 32, hkv, hd)
+    positive_keys(cache)
+    check_prompt(cache, (sign * 60 * (1 + 0.05 * rng.normal(size=(3, 40, hq, hd)))).astype(np.float32), lens, window, sinks, 2, f"far {sign}")
+
+
+@pytest.mark.parametrize("hd,hq,hkv", [(32, 4, 2), (64, 8, 2), (128, 8, 2)])
 @pytest.mark.parametrize("sign", [-1, 1])
 def test_prompts_whose_far_scores_almost_tie(hd, hq, hkv, sign):
     """Every token sees two keys whose scores, some hundreds from 0, differ by about 1:
