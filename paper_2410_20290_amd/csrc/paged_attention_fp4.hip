@@ -95,7 +95,7 @@ __device__ __forceinline__ RowState uniform(const RowState& r) { return {uniform
 // of its probabilities, at no product more; else every part takes products of its own (of
 // probabilities in bf16 there is one then).  Probabilities in two parts against one: 5
 // rows of 30-60k keys 60 us for 60, outputs 0.0017 (their own rounding) off in the 2-norm
-// for 0.0022; 512 rows on 1024 shared keys 72 us for 71.5.
+// for 0.0022; 512 rows on 1024 shared keys 71.6 us for 70.9.
 template <bool F32, int SPREAD>
 struct Fp4Parts {
   static constexpr int COLS = 16 / SPREAD;
@@ -345,8 +345,9 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
       float pv = __builtin_amdgcn_exp2f(sv[i] - m);
       ps += pv;
       if constexpr (SPREAD > 1) {
+        const float first = __uint_as_float(__float_as_uint(pv) & 0xFFFF0000u);   // (cut, for one instruction)
         if constexpr (F32) pf[0][i] = my_part<SPREAD, 3>(pv, part);
-        else pf[0][i] = (__bf16)(part == 0 ? pv : pv - (float)(__bf16)pv);
+        else pf[0][i] = (__bf16)(part == 0 ? first : pv - first);
       } else {
         __bf16 p[PSETS];
         in_parts<PSETS>(pv, p);
