@@ -15,7 +15,7 @@
  * scale.  b = 255: every value of the group is NaN.  The operators write the
  * least b with which the group's largest magnitude is below 7 scales (2 where it
  * is 0, 252 where it is 2^127 or more), the nearest values, ties to the even
- * code, magnitudes from 5 scales on as 6; a group that holds a NaN or an infinity
+ * code, magnitudes above 5 scales as 6; a group that holds a NaN or an infinity
  * gets b = 255 and codes 0.  On normal draws the values are 11 % off in the
  * 2-norm.
  * A layer's block of keys (or values) is laid out [n_pages][n_kv_heads], each of
@@ -71,7 +71,7 @@ sr_status sr_page_read(int32_t cache, int32_t dtype, int32_t head_dim, int32_t n
  * pages stand for.  out: dtype SR_BF16 or SR_F32.  On the matrix cores, which keys
  * and values enter exactly.  SR_BF16: queries keep 16 bits where a row has at most 16
  * query columns (lr n_heads / n_kv_heads), and where it has more are off by up to 2^-13
- * of the largest of every 32 dimensions; probabilities keep 16 bits where a row has at
+ * of the largest of every 32 dimensions (products of such a query with keys are exact); probabilities keep 16 bits where a row has at
  * most 8 columns, 8 where it has more and for shared keys that are read once for all
  * rows; sums are in fp32.  SR_F32: queries and probabilities enter as three parts, all
  * 24 bits.  A layer's keys take less than
