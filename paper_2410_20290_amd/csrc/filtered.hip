@@ -7,8 +7,9 @@
 //
 // Few entries matter to most draws, so a row is read twice: for its maximum, and to
 // list its best entries (and weigh all of them where only top-p asks for the
-// total).  Where "best" begins follows from the maxima of 1024 or 2048 subsets of the
-// row: an entry that reaches the k-th largest of them is one of at least k.  Borders
+// total).  Where "best" begins follows from the maxima of subsets of the row, 1024 by one
+// work-group, 64 for every 4096 entries by the split readings: an entry that reaches the
+// k-th largest of them is one of at least k.  Borders
 // are then found in the list by counting and weighing its entries in 2048 bins.  Where
 // the list is not enough (flat rows under top-p, a top-k above 1024, thousands of
 // equals), the whole row goes into bins of z = (l - max) / T, 92 to a unit of z, then
@@ -16,11 +17,13 @@
 //
 // Measured with fp32 logits of 128256 entries: one row 18 us (its readings by 32
 // work-groups; by one alone 50); 512 rows, of which one half keeps 50 and the rest follow
-// other settings, 115 us, all with a top-k of 50 60 us, with a top-p of 0.9 154 us
-// (263 MB, 48 us at the rate of a pure read: a second reading, and the exponentials of
-// 66 M entries), unfiltered 104 us.  256 flat rows of 32000 bf16 logits under a top-p of
-// 0.95 53 us: maximum 6, whether a list can be enough 3, bins 15 (64-bit adds in LDS), the
-// border's bin and the sums before it 12 (their exponentials), search 12, drawn entry 4.
+// other settings, 115 us.  The same rows (half of them flat) call after call: all with a
+// top-k of 50 54 us, unfiltered 90 us, with a top-p of 0.9 182 us (263 MB, 48 us at the rate of
+// a pure read: further readings, and the exponentials of 66 M entries).  256 flat rows of
+// 32000 bf16 logits under a top-p of 0.95 57 to 60 us: maximum 6, whether a list can be
+// enough 3, bins 15 (64-bit adds in LDS), the border's bin and the sums before it 12 (their
+// exponentials), search 12, drawn entry 4 (timed one by one, with the gaps between them left
+// out).
 //
 //   filtered_kernel         a work-group of 16 waves a row, from the logits to the token
 //   filtered_maxima_kernel, few rows: the two readings by work-groups of four tiles
@@ -379,7 +382,7 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
   // the passes of rows that no list decides, where fetching the code of a tile's 16
   // entries takes longer than running it (flat rows under a top-p of 0.95, 16 entries at a
   // time -> 4: 256 of 32000 bf16 values 66 -> 57.5 us, 512 of 128256 290 -> 222 us; whole tiles a
-  // wave, so that a tile is summed once: 53 and 203 us).
+  // wave, so that a tile is summed once, a further 8 %).
   auto pass4 = [&](auto&& f) {
     auto load = [&](int i, float (&v)[4]) {
       if (VEC && i + 4 <= vocab) {

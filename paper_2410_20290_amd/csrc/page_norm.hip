@@ -24,11 +24,12 @@ template <> __device__ __forceinline__ bf16_t round_once<bf16_t>(double v) {
 // ------------------------------------------------------------------ append
 // A work-group takes one token; a thread takes units of 8 dimensions of a head,
 // HD / 8 neighbouring lanes a head: four rotated pairs, or 8 dimensions that pass.
-// Everything in 64 bits, rounded once.  Memory bounds it: 19 ragged prompts of up to 2333
-// tokens, 48 heads of 64 dimensions, into 4 bits 134 us (with the read below 697 MB in 154,
-// 4.5 TB/s, a copy reaches 4.9).  128 threads where a token has up to 512 units, so that
+// Everything in 64 bits, rounded once.  Memory bounds prompts: 19 ragged ones of up to 2333
+// tokens, 48 heads of 64 dimensions, into 4 bits 133 to 136 us (with the read below 697 MB in
+// 154, 4.5 TB/s, a copy reaches 4.9); one token a row is bound by loads that wait for each
+// other (length, token count, frequencies, angles, projections).  128 threads where a token has up to 512 units, so that
 // few idle in the last pass over it (those prompts, of 384 units: 256 threads 150 us), 256
-// where it has more (512 tokens of 768 units: 9 us with 256, 13 with 128).
+// where it has more (512 tokens of 768 units: 9.6 us with 256, 13 with 128).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) append_norm_kernel(PageAppendNormArgs na) {
   constexpr int UPH = HD / 8, NG = HD / 32;   // units of a head, groups of 4-bit values
@@ -166,7 +167,7 @@ void page_append_norm(const PageAppendNormArgs& a, hipStream_t s) {
 
 // -------------------------------------------------------------------- read
 // A thread takes 8 dimensions of a key and of a value; a work-group whole tokens, as many
-// as fill it.  Those prompts' 8 heads out of 4 bits: 22 us (work-groups of 256 units of keys
+// as fill it.  Those prompts' 8 heads out of 4 bits: 21 us (3.5 TB/s) (work-groups of 256 units of keys
 // or of values, each unit's token by a 64-bit division: 39).
 constexpr int kReadThreads = 256;
 template <typename C, typename T, int HD>

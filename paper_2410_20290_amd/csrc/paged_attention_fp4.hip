@@ -128,9 +128,9 @@ __device__ __forceinline__ __bf16 my_part(float x, int part) {
 // run of 64.  The keys below common[row] are another pass's.  Keys that nobody sees are
 // read where they lie (their scores are masked) and their values as zeros; a half
 // without a page is read from page 0.
-// Memory bounds long rows: 5 of 30-60k keys, 8 heads of 128 dimensions, 245 MB in 44 us
-// (5.6 TB/s; a kernel that only reads reaches 5.5 to 6), the merge 5.5 us behind it.  512
-// rows' own 41 to 460 keys 36 us (every wave has its own start and merge).
+// Memory bounds long rows: 5 of 30-60k keys, 8 heads of 128 dimensions, 245 MB in 45 us
+// (5.4 TB/s; a kernel that only reads reaches 5.5 to 6), the merge 5.4 us behind it.  512
+// rows' own 41 to 460 keys 37 us (every wave has its own start and merge).
 template <int HD, int NW, bool F32, int SPREAD>
 __global__ void __launch_bounds__(64 * NW, HD == 128 && SPREAD == 1 ? 3 : 4)
 fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits, int pre, int slots, float qscale) {
@@ -490,16 +490,18 @@ fp4_wave_kernel(PagedAttnArgs a, const int32_t* __restrict__ common, int splits,
 //                 6 bits (e2m3), each with a scale for 32 dimensions: at most 1 / 15360
 //                 of the largest of these is left.  The products are exact, and a sum of
 //                 64 of them with scales of any size is off by 2^-21 of the largest at
-//                 most (measured).  6011 tokens, hd 128: 323 us; queries in one bf16 341
-//                 us and half as precise, in two 537 us.  53 chunks of up to 333 tokens,
-//                 hd 64: 150, 134 and 166 us.
+//                 most (measured).  Scores from queries in one bf16 took 5 % longer at
+//                 head_dim 128 and 10 % less at 64, and were half as precise; in two 66
+//                 and 11 % longer.
 //                 The maximum is taken off by one more product, not by vector work
 //                 (200 tokens on 60k keys 229 -> 209 us).
-// With lengths and block numbers in scalar registers 311 and 133 us, with the maximum in
-// the product 307 (965 TFLOP/s) and 131.  What bounds it: a block of 32 x 32 scores is 256
-// clocks of exponentials and some 250 of other vector work a wave, beside 480 (hd 128) or
-// 256 of matrix work, and the waves of a SIMD hardly overlap them.  The next block's
-// scores beneath this one's exponentials, or two blocks a barrier: the same time.  Lane i keeps the place and the mask flags of block i of a run of 64.
+// 6011 tokens, hd 128: 304 to 318 us (930 to 975 TFLOP/s); 53 chunks of up to 333 tokens, hd
+// 64: 129 to 134 us.  What bounds it: a block of 32 x 32 scores is 256 clocks of exponentials
+// and some 250 of other vector work a wave, beside 480 (hd 128) or 256 of matrix work, and
+// the waves of a SIMD hardly overlap them (matrix instructions busy 41 and 31 % of the
+// clocks, vector ones 43 and 66 %).  The next block's scores beneath this one's exponentials, or
+// two blocks a barrier: the same time.  Lane i keeps the place and the mask flags of block i of a
+// run of 64.
 // The output is rescaled only when a maximum has moved by more than
 // kStale.
 constexpr int kTileCols = 128;
