@@ -477,7 +477,9 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
   const int whole = min(kFltWaves, vocab / kLpTile);
   const bool by_list = (rd.by_k && (rd.k <= 64 * whole || vocab <= kFltList)) || (!rd.by_k && rd.by_p);
   const bool at_once = !SPLIT && rd.by_k && !rd.greedy && rd.k <= kFltThreads && vocab >= 2 * kFltWaves * kLpTile;
-  float from = -FLT_MAX, highest = -FLT_MAX, own = kMasked;   // (own: of the wave)
+  float from = -FLT_MAX, highest = -FLT_MAX;
+  float own = kMasked;   // the wave's bound, and the tile from which on it holds
+  int since = 0;
   if (tid == 0) sh.n = 0;
   __syncthreads();
   {
@@ -493,6 +495,7 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
           if (own == kMasked) {   // (uniform)
             first = reached(key_of(mt), min(64, 8 + (int)(2 * (int64_t)rd.k * kLpTile / vocab)));
             own = uniform(fmaxf(value_of(first), kMasked));
+            since = base;
           }
           list_those(v, base, [&](float l) { return l >= own; });
         }
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
 
   // The list of the best, where it can be enough: that of the first pass, or ...
   float lo = from, hi = INFINITY;   // (another pass lists from lo on, below hi, ...)
-  bool again = true;                // (... from the start, not beside what is listed)
+  bool again = true;                // (... from the start, not what the first one left out)
   if (at_once && !infinite) {
     const int n = sh.n;
     if (n <= kFltList && n >= rd.k) {
@@ -599,13 +602,14 @@ __global__ void __launch_bounds__(kFltThreads, 8) filtered_kernel(FilteredArgs a
       __syncthreads();
       if (again) {
         end = rd.place(from);
+        since = 0;
         if (tid == 0) sh.n = 0;
         __syncthreads();
       }
       if (lo < hi)
         pass([&](const float(&v)[16], int base) {
           if (weigh) total += rd.weights(v, [](int, uint32_t) { return true; });
-          list_those(v, base, [&](float l) { return (l >= lo) & (l < hi); });
+          if (base >= since) list_those(v, base, [&](float l) { return (l >= lo) & (l < hi); });
         });
       total = block_scan(total, sh).all;   // (and every entry is listed)
       n = sh.n;

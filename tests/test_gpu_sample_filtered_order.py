@@ -12,7 +12,7 @@ from test_gpu_sample_filtered import check
 pytestmark = pytest.mark.gpu
 
 KINDS = ["falls", "falls fast", "rises", "one tile", "first tile", "masked -inf", "masked lowest", "masked finite", "all but one masked",
-         "few left", "falls in steps"]
+         "few left", "falls in steps", "lowest everywhere", "lowest but 60"]
 
 
 def ordered(rng, vocab, kind):
@@ -38,6 +38,10 @@ def ordered(rng, vocab, kind):
         x[:], x[vocab - 7] = low, 1.0
     elif kind == "few left":
         x[3000:] = -np.inf
+    elif kind.startswith("lowest"):
+        x[:] = low
+        if kind == "lowest but 60":
+            x[rng.integers(0, vocab, 60)] = rng.normal(0, 2, 60)
     elif kind == "falls in steps":
         x = np.floor(8 - np.log2(1 + i))
     return x.astype(np.float32)
@@ -50,7 +54,7 @@ def test_logits_that_depend_on_the_index(vocab, bf16):
     rng = np.random.default_rng(vocab)
     rows = 132
     x = np.full((rows, vocab), -np.inf, np.float32)
-    for r in range(rows if vocab < 100000 else 33):    # (the others: nothing allowed)
+    for r in range(rows if vocab < 100000 else 39):    # (the others: nothing allowed)
         x[r] = ordered(rng, vocab, KINDS[r % len(KINDS)])
     t = torch.from_numpy(x).cuda()
     if bf16:
